@@ -32,7 +32,8 @@
  *    buffers, sources, q/k_new/v_new/out, mask, workspace).  The library owns
  *    only the host handle and never allocates device memory.  Device buffers
  *    must stay valid until the stream has passed the call that uses them.
- *  - Element types: fp32 or bf16 storage, fp32 arithmetic.  head_dim 64 or 128;
+ *  - Element types: fp32 or bf16 storage, fp32 arithmetic; or a cache held in 4
+ *    bits under bf16 inputs and outputs (BATON_MXFP4).  head_dim 64 or 128;
  *    n_q_heads / n_kv_heads in {1, 2, 4, 8}; batch <= BATON_MAX_BATCH.
  *
  * Memory layout (device).  K and V are each
@@ -48,6 +49,23 @@
  * baton_kv_evict).  An eviction without BATON_SCRUB leaves its query's tokens
  * in place as stale bytes; no kernel ever reads a position that is not a live
  * token, so results do not depend on what such positions hold.
+ *
+ * A cache held in 4 bits (BATON_MXFP4) takes 17/64 of the bytes of a bf16 one.
+ * 32 consecutive elements of a token's head share a scale byte s; an element is a
+ * 4-bit code: a sign (the high bit) and 0, 1/2, 1, 3/2, 2, 3, 4 or 6 times
+ * 2^(s - 127).  K and V are each [n_layers][batch][n_kv_heads] rows of capacity *
+ * (head_dim / 2 + head_dim / 32) bytes: the codes [capacity][head_dim / 2], two to
+ * a byte, the first in the low half, then the scales [capacity][head_dim / 32];
+ * capacity is a multiple of 16.  Sources, destinations, q, k_new, v_new and out
+ * are bf16.  Keys and values are rounded as they are stored (embedded, or appended
+ * by a step): the scale is the smallest power of two, from 2^-125 to 2^125, that
+ * takes the block's largest magnitude to at most 7, the code the nearest one (ties
+ * to even); a block that holds an infinity or a NaN is stored as NaN (s = 255).
+ * Extracting a query gives the values it is stored as, and embedding those stores
+ * the same bits again, so everything said about extract, embed and move holds bit
+ * for bit.  In the step that brings them, keys and values take part in attention
+ * as given; rounded in every later one.  A placeholder is the low 8 bits of
+ * fill_bits in every byte of a token's codes and scales.
  */
 #ifndef BATON_H
 #define BATON_H
@@ -73,11 +91,16 @@ typedef enum baton_status {
   BATON_ESCRATCH = 7   /* baton_decode_attn_noalloc: the step needs more than BATON_SCRATCH_BYTES */
 } baton_status;
 
-typedef enum baton_dtype { BATON_F32 = 0, BATON_BF16 = 1 } baton_dtype;
+typedef enum baton_dtype {
+  BATON_F32 = 0,
+  BATON_BF16 = 1,
+  BATON_MXFP4 = 2 /* a cache's K and V in 4 bits; all else bf16 */
+} baton_dtype;
 
 /* The paper's placeholder value, -inf (sec. 4.1, KV_Cache paragraph; sec. 4.2). */
 #define BATON_FILL_NEG_INF_F32 0xFF800000u
 #define BATON_FILL_NEG_INF_BF16 0xFF80u
+#define BATON_FILL_NAN_MXFP4 0xFFu /* 4 bits have no infinity: every scale NaN */
 
 #define BATON_MAX_BATCH 512
 #define BATON_MAX_PREFILL 64 /* queries prefilled inside the batch in one step */
@@ -91,17 +114,19 @@ typedef enum baton_dtype { BATON_F32 = 0, BATON_BF16 = 1 } baton_dtype;
 #define BATON_SCRUB 2u   /* overwrite the finished queries' tokens with the placeholder */
 
 typedef struct baton_cache_desc {
-  int32_t dtype;      /* baton_dtype of K, V, sources, q, k_new, v_new and out */
+  int32_t dtype;      /* baton_dtype of K, V, sources, q, k_new, v_new and out
+                         (BATON_MXFP4: of K and V, the rest bf16) */
   int32_t n_layers;   /* >= 1 */
   int32_t batch;      /* slots, 1 .. BATON_MAX_BATCH */
   int32_t n_q_heads;  /* query heads per layer */
   int32_t n_kv_heads; /* key/value heads per layer (n_q_heads / n_kv_heads in {1,2,4,8}) */
   int32_t head_dim;   /* 64 or 128 */
-  int64_t capacity;   /* ring columns per row, >= 2 */
+  int64_t capacity;   /* ring columns per row, >= 2 (BATON_MXFP4: a multiple of 16) */
   void* k;            /* device, [n_layers][batch][n_kv_heads][capacity][head_dim], 16-byte aligned;
-                         layer l's rows (dense) at k + l * layer_stride elements */
+                         layer l's rows (dense) at k + l * layer_stride elements
+                         (BATON_MXFP4: rows of codes and scales, layer_stride in bytes) */
   void* v;            /* device, same layout as k */
-  uint32_t fill_bits; /* placeholder bit pattern in the low 32 (fp32) or 16 (bf16) bits */
+  uint32_t fill_bits; /* placeholder bit pattern in the low 32 (fp32), 16 (bf16) or 8 (4-bit) bits */
   int64_t layer_stride; /* elements from layer l's rows to layer l + 1's, in k and in v alike;
                            0: packed (batch * n_kv_heads * capacity * head_dim).  A larger
                            stride lets K and V share one allocation interleaved by layer,
@@ -120,7 +145,8 @@ typedef struct baton_cache baton_cache; /* opaque host handle */
  * fill_bits over all of K and V.  The descriptor is copied.
  * Errors: EINVAL (null out/k/v, sizes out of range, misaligned k/v,
  * layer_stride below one layer's rows or not a whole number of 16-byte
- * vectors, k and v overlapping), EDTYPE (dtype, head_dim or grouping
+ * vectors, k and v overlapping, BATON_MXFP4 with a capacity that is no multiple
+ * of 16), EDTYPE (dtype, head_dim or grouping
  * unsupported), EHIP.
  */
 baton_status baton_cache_create(const baton_cache_desc* desc, uint32_t flags, hipStream_t stream,
@@ -263,7 +289,8 @@ size_t baton_decode_attn_workspace_bytes(const baton_cache* cache);
  * over the slot's own columns j in [L - len_b, L] only; placeholder columns
  * are skipped, never read into arithmetic.  Free slots: nothing appended, out
  * rows set to 0.  Arithmetic in fp32; out rounded to nearest-even in the
- * cache's dtype.
+ * cache's dtype (bf16 over a cache in 4 bits, where the softmax weights are
+ * rounded to bf16 for their product with the values, their sum in fp32).
  * Live rows' holes are skipped like placeholders.
  * q, out: device [batch][n_q_heads][head_dim]; k_new, v_new: device
  * [batch][n_kv_heads][head_dim]; all 16-byte aligned.
@@ -459,7 +486,7 @@ baton_status baton_rmsnorm(int32_t dtype, const void* x, const void* gain, void*
  * pos_b * theta^(-2i/head_dim), pos_b = slot b's token count
  * (baton_cache_tokens), the position of the token being decoded.  The angles
  * are formed and reduced modulo 2 pi in double precision.  Decode steps only.
- * Errors: EINVAL (null pointer, theta <= 1), EDTYPE (cache not bf16), ESTATE
+ * Errors: EINVAL (null pointer, theta <= 1), EDTYPE (fp32 cache), ESTATE
  * (a prefill is registered), EHIP.
  */
 baton_status baton_rope_qkv(const baton_cache* cache, const void* qkv, void* q, void* k_new, void* v_new,

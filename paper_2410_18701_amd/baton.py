@@ -18,9 +18,10 @@ STATUS_NAMES = ["BATON_OK", "BATON_EINVAL", "BATON_ESLOT", "BATON_ECAPACITY", "B
                 "BATON_ESTATE", "BATON_EHIP", "BATON_ESCRATCH"]
 BATON_SCRATCH_BYTES = 64 << 20
 BATON_GEMM_MAX_ROWS = 256
-BATON_F32, BATON_BF16 = 0, 1
+BATON_F32, BATON_BF16, BATON_MXFP4 = 0, 1, 2
 BATON_FILL_NEG_INF_F32 = 0xFF800000
 BATON_FILL_NEG_INF_BF16 = 0xFF80
+BATON_FILL_NAN_MXFP4 = 0xFF
 BATON_MAX_BATCH = 512
 BATON_MAX_PREFILL = 64
 BATON_MAX_HOLES = 64

@@ -5,13 +5,33 @@ the C ABI (paper_2410_18701_amd/baton.py).
 """
 from . import baton as B
 
-_DTYPE_CODE = {"f32": B.BATON_F32, "bf16": B.BATON_BF16}
-_FILL = {"f32": B.BATON_FILL_NEG_INF_F32, "bf16": B.BATON_FILL_NEG_INF_BF16}
+_DTYPE_CODE = {"f32": B.BATON_F32, "bf16": B.BATON_BF16, "mxfp4": B.BATON_MXFP4}
+_FILL = {"f32": B.BATON_FILL_NEG_INF_F32, "bf16": B.BATON_FILL_NEG_INF_BF16, "mxfp4": B.BATON_FILL_NAN_MXFP4}
 
 
 def torch_dtype(dtype):
+    """Element type of sources, queries and outputs (and of K and V unless held in 4 bits)."""
     import torch
     return torch.float32 if dtype == "f32" else torch.bfloat16
+
+
+def row_bytes_mxfp4(capacity, head_dim):
+    """Bytes of a row of K or V held in 4 bits: codes, then scales."""
+    return capacity * (head_dim // 2 + head_dim // 32)
+
+
+def unpack_mxfp4(rows, capacity, head_dim):
+    """The bf16 values of rows [...][row bytes] of a 4-bit ring: [...][capacity][head_dim]
+    (a copy; NaN where a scale is NaN)."""
+    import torch
+    codes, scales = rows.split([capacity * (head_dim // 2), capacity * (head_dim // 32)], dim=-1)
+    lead = rows.shape[:-1]
+    c = torch.stack([codes & 15, codes >> 4], -1).reshape(*lead, capacity, head_dim // 32, 32).int()
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=rows.device)
+    v = torch.where(c > 7, -grid[c & 7], grid[c & 7])
+    s = scales.reshape(*lead, capacity, head_dim // 32, 1).int()
+    v = torch.where(s == 255, float("nan"), torch.ldexp(v, s - 127))
+    return v.reshape(*lead, capacity, head_dim).to(torch.bfloat16)
 
 
 def _cur_stream():
@@ -29,7 +49,8 @@ class BatonCache:
     """A batch of `batch` slots over a K/V ring of `capacity` columns per row.
 
     k, v: [n_layers][batch][n_kv_heads][capacity][head_dim] device tensors,
-    each layer dense.  Unless given, they are made with layout "by_layer" --
+    each layer dense; with dtype "mxfp4" (held in 4 bits, sources, queries and
+    outputs bf16) [n_layers][batch][n_kv_heads][row_bytes_mxfp4] bytes.  Unless given, they are made with layout "by_layer" --
     views of one [n_layers][2][batch][n_kv_heads][capacity][head_dim] tensor,
     K and V of a layer next to each other (the library streams them about 4%
     faster than from two allocations) -- or "separate" (two tensors).
@@ -43,8 +64,11 @@ class BatonCache:
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         self.capacity = capacity
         self.fill_bits = _FILL[dtype] if fill_bits is None else fill_bits
-        tdt = torch_dtype(dtype)
-        shape = (n_layers, batch, n_kv_heads, capacity, head_dim)
+        self.io_dtype = torch_dtype(dtype)   # of sources, queries and outputs
+        if dtype == "mxfp4":
+            tdt, shape = torch.uint8, (n_layers, batch, n_kv_heads, row_bytes_mxfp4(capacity, head_dim))
+        else:
+            tdt, shape = self.io_dtype, (n_layers, batch, n_kv_heads, capacity, head_dim)
         if (k is None) != (v is None):
             raise ValueError("give both k and v, or neither")
         if k is None:
@@ -115,8 +139,8 @@ class BatonCache:
         ks, vs = [], []
         for s in slots:
             shape = (self.n_layers, self.n_kv_heads, max(lens[s], 0), self.head_dim)
-            ks.append(torch.empty(shape, dtype=self.k.dtype, device=self.k.device))
-            vs.append(torch.empty(shape, dtype=self.k.dtype, device=self.k.device))
+            ks.append(torch.empty(shape, dtype=self.io_dtype, device=self.k.device))
+            vs.append(torch.empty(shape, dtype=self.io_dtype, device=self.k.device))
         B.baton_kv_extract(self.handle, slots, ks, vs, stream if stream is not None else _cur_stream())
         return ks, vs
 
@@ -139,8 +163,8 @@ class BatonCache:
         want_kv = self.batch * T * self.n_kv_heads * self.head_dim
         for name, t, n in (("q", q, want_q), ("k_new", k_new, want_kv), ("v_new", v_new, want_kv),
                            ("out", out, want_q)):
-            if t.dtype != self.k.dtype or not t.is_contiguous() or t.numel() != n:
-                raise ValueError(f"{name}: expected {n} contiguous {self.k.dtype} elements, "
+            if t.dtype != self.io_dtype or not t.is_contiguous() or t.numel() != n:
+                raise ValueError(f"{name}: expected {n} contiguous {self.io_dtype} elements, "
                                  f"got {t.numel()} {t.dtype}")
         ws = self.workspace()
         B.baton_decode_attn(self.handle, layer, q, k_new, v_new, out, scale, ws, ws.numel(),
@@ -160,10 +184,13 @@ class BatonCache:
         return B.baton_cache_query(self.handle, self.batch)
 
     def logical(self, which="k"):
-        """The aligned cache [layer][batch][head][L][dim] read off the ring (a copy)."""
+        """The aligned cache [layer][batch][head][L][dim] read off the ring (a copy;
+        of a cache held in 4 bits, the values it stands for)."""
         import torch
         L, base, _ = self.query()
         buf = self.k if which == "k" else self.v
+        if self.dtype == "mxfp4":
+            buf = unpack_mxfp4(buf, self.capacity, self.head_dim)
         idx = (torch.arange(L, device=buf.device) + base) % self.capacity
         return buf.index_select(3, idx)
 

@@ -14,6 +14,8 @@
 #include "decode_attn.hpp"
 #include "decode_attn_mfma.hpp"
 #include "kv_ops.hpp"
+#include "kv4_ops.hpp"
+#include "decode_attn_kv4.hpp"
 #include "layer_ops.hpp"
 #include "prefill_attn.hpp"
 #include "prefill_plan.hpp"
@@ -42,7 +44,7 @@ struct baton_hole {
 
 struct baton_cache {
   baton_cache_desc d;
-  int32_t esz;             // bytes per element
+  int32_t esz;             // bytes per element of the inputs (and of K and V, unless held in 4 bits)
   int32_t vpt;             // 16-byte vectors per token row
   int32_t group;           // q-heads per kv-head
   int32_t split;           // tokens per attention work item; 0: chosen per step
@@ -88,6 +90,7 @@ using baton::SegArgs;
 
 uint32_t fill_word(const baton_cache* c) {
   if (c->esz == 4) return c->d.fill_bits;
+  if (c->d.dtype == BATON_MXFP4) return (c->d.fill_bits & 0xFFu) * 0x01010101u;
   const uint32_t h = c->d.fill_bits & 0xFFFFu;
   return h | (h << 16);
 }
@@ -155,6 +158,8 @@ struct Seg {
   int32_t dst_slot = -1; // a move: the slot receiving the columns
 };
 
+#include "kv4_launch.hpp"   // the same for a cache held in 4 bits, and its decode attention's launches
+
 template <int VPT>
 baton_status launch_segs_vpt(const baton_cache* c, const std::vector<Seg>& segs, int mode,
                              hipStream_t s) {
@@ -205,6 +210,7 @@ baton_status launch_segs_vpt(const baton_cache* c, const std::vector<Seg>& segs,
 // mode: 0 copy into the ring (or placeholders), 1 copy out of it, 2 row to row.
 baton_status launch_segs(const baton_cache* c, const std::vector<Seg>& segs, hipStream_t s,
                          int mode = 0) {
+  if (is_kv4(c)) return launch_segs4(c, segs, mode, s);
   switch (c->vpt) {
     case 8: return launch_segs_vpt<8>(c, segs, mode, s);
     case 16: return launch_segs_vpt<16>(c, segs, mode, s);
@@ -233,7 +239,9 @@ template <int D, int G>
 void launch_prefill_g(const baton_cache* c, baton::PrefillArgs& a, hipStream_t s) {
   int32_t longest = 0;
   for (int32_t i = 0; i < a.n_ins; ++i) longest = std::max(longest, a.plen[i]);
-  auto grid = [&] { return dim3((unsigned)((int64_t)a.n_tiles * (c->d.n_q_heads + c->d.n_kv_heads))); };   // and the append workgroups
+  // and the append workgroups, unless the prompts are stored in 4 bits (append_prompts4)
+  const int32_t per_tile = c->d.n_q_heads + (is_kv4(c) ? 0 : c->d.n_kv_heads);
+  auto grid = [&] { return dim3((unsigned)((int64_t)a.n_tiles * per_tile)); };
   prefill_tiles(c, a, baton::kPrefillTile32);
   if (baton::prefill_long(D, a.plen, a.n_ins, a.n_attn)) {
     hipLaunchKernelGGL((baton::prefill_fa32_kernel<D, G>), grid(), dim3(256), 0, s, a);
@@ -413,7 +421,7 @@ baton_status attn_run(baton_cache* c, int32_t layer, const void* q, const void* 
   a.tw = c->step_T;
   const float sc = scale == 0.f ? 1.0f / std::sqrt((float)c->d.head_dim) : scale;
   a.qscale = sc * 1.4426950408889634f;
-  if (c->n_items > 0 && !launch_attn(c, a, stream)) return BATON_EDTYPE;
+  if (c->n_items > 0 && !(is_kv4(c) ? launch_attn4(c, a, stream) : launch_attn(c, a, stream))) return BATON_EDTYPE;
   baton_status st = hip_status(hipGetLastError());
   if (st != BATON_OK) return st;
   if (c->n_prefill > 0) {
@@ -446,6 +454,7 @@ baton_status attn_run(baton_cache* c, int32_t layer, const void* q, const void* 
     if (c->d.head_dim == 64) launch_prefill_d<64>(c, p, stream);
     else launch_prefill_d<128>(c, p, stream);
     st = hip_status(hipGetLastError());
+    if (st == BATON_OK && is_kv4(c)) st = append_prompts4(c, p, stream);
     if (st != BATON_OK) return st;
   }
   c->layer_done[layer] = 1;
@@ -500,7 +509,7 @@ baton_status baton_cache_create(const baton_cache_desc* desc, uint32_t flags, hi
   if (!desc || !out) return BATON_EINVAL;
   if (flags & ~BATON_CREATE_ASSUME_FILLED) return BATON_EINVAL;
   const baton_cache_desc& d = *desc;
-  if (d.dtype != BATON_F32 && d.dtype != BATON_BF16) return BATON_EDTYPE;
+  if (d.dtype != BATON_F32 && d.dtype != BATON_BF16 && d.dtype != BATON_MXFP4) return BATON_EDTYPE;
   if (d.head_dim != 64 && d.head_dim != 128) return BATON_EDTYPE;
   if (d.n_layers < 1 || d.batch < 1 || d.batch > BATON_MAX_BATCH || d.n_q_heads < 1 ||
       d.n_kv_heads < 1 || d.capacity < 2 || d.capacity > (int64_t(1) << 31))
@@ -509,15 +518,20 @@ baton_status baton_cache_create(const baton_cache_desc* desc, uint32_t flags, hi
   const int32_t g = d.n_q_heads / d.n_kv_heads;
   if (g != 1 && g != 2 && g != 4 && g != 8) return BATON_EDTYPE;
   if (!d.k || !d.v || !aligned16(d.k) || !aligned16(d.v)) return BATON_EINVAL;
-  const int64_t esz = d.dtype == BATON_F32 ? 4 : 2;
+  const bool kv4 = d.dtype == BATON_MXFP4;
+  // rows in 4 bits are whole 16-byte vectors from multiples of 16 columns on
+  if (kv4 && d.capacity % 16) return BATON_EINVAL;
+  // bytes of what a row's, a layer's and the stride's elements count: 4-bit rows in bytes
+  const int64_t esz = kv4 ? 1 : d.dtype == BATON_F32 ? 4 : 2;
+  const int64_t row_elems = kv4 ? baton::kv4_row_bytes(d.capacity, d.head_dim) : d.capacity * d.head_dim;
   // a row of the ring is addressed with 32-bit byte offsets
-  if (d.capacity * d.head_dim * esz >= (int64_t(1) << 31)) return BATON_EINVAL;
+  if (row_elems * esz >= (int64_t(1) << 31)) return BATON_EINVAL;
   // One layer's rows, [batch][n_kv_heads][capacity][head_dim], are dense; the
   // layers are layer_stride elements apart (0: packed), a whole number of
   // 16-byte vectors, and K's and V's layers must not overlap.
   // Sizes are bounded first so that the byte arithmetic below cannot
   // overflow: K (and V) must span less than 2^56 bytes.
-  const __int128 layer_elems_w = (__int128)d.batch * d.n_kv_heads * d.capacity * d.head_dim;
+  const __int128 layer_elems_w = (__int128)d.batch * d.n_kv_heads * row_elems;
   if (d.layer_stride < 0 || layer_elems_w * esz >= ((__int128)1 << 56)) return BATON_EINVAL;
   const int64_t layer_elems = (int64_t)layer_elems_w;
   const int64_t stride = d.layer_stride == 0 ? layer_elems : d.layer_stride;
@@ -547,7 +561,7 @@ baton_status baton_cache_create(const baton_cache_desc* desc, uint32_t flags, hi
   c->plen.assign(d.batch, 0);
   c->layer_done.assign(d.n_layers, 0);
   if (!(flags & BATON_CREATE_ASSUME_FILLED)) {
-    const int64_t n_vec = (int64_t)d.batch * d.n_kv_heads * d.capacity * c->vpt;   // per layer
+    const int64_t n_vec = layer_elems * esz / 16;   // per layer
     const int64_t gy = std::min<int64_t>(d.n_layers, 65535);
     const int64_t bx = std::max<int64_t>(1, std::min<int64_t>((n_vec + 255) / 256, (256 * 64 + gy - 1) / gy));
     hipLaunchKernelGGL(baton::fill_kernel, dim3((unsigned)bx, (unsigned)gy), dim3(256), 0, stream,
@@ -888,7 +902,7 @@ baton_status baton_cache_tokens(const baton_cache* c, int32_t* tokens) {
 baton_status baton_rope_qkv(const baton_cache* c, const void* qkv, void* q, void* k_new, void* v_new,
                             float theta, hipStream_t stream) {
   if (!c || !qkv || !q || !k_new || !v_new || !(theta > 1.f) || !std::isfinite(theta)) return BATON_EINVAL;
-  if (c->d.dtype != BATON_BF16) return BATON_EDTYPE;
+  if (c->d.dtype == BATON_F32) return BATON_EDTYPE;
   if (c->n_prefill) return BATON_ESTATE;   // decode steps only
   baton::RopeArgs a;
   std::memset(&a, 0, sizeof(a));

@@ -1,0 +1,308 @@
+// Decode attention over a cache held in 4 bits (kv4_ops.hpp has the format), on
+// the matrix cores, for every grouping.  Work items, partial records and their
+// merge are those of the bf16 kernels.
+//
+// What bounds it is HBM -- 68 bytes of K or V per token at head_dim 128, against
+// 256 in bf16 -- as long as turning codes into operands costs few instructions:
+// a wave that streams its share of 8 TB/s has about 40 vector instructions per
+// token row pair and 64 lanes.  Per iteration a wave takes 64 tokens:
+//  * QK^T: A = 16 key rows x 32 of d, four tiles of 16 consecutive tokens.  The
+//    contraction's order is free, so lane l takes the D / 4 elements from D / 4 *
+//    (l / 16) on of its key row -- one load of 16 bytes (8 at head_dim 64), a
+//    quarter row, all in one scale block -- and the query is laid out the same
+//    way.  No key passes through LDS; one instruction turns two codes and the
+//    block's scale into two bf16 of the operand, exactly.
+//  * the scores of tile j, row 4 g + r are lane group g's register (j, r), so a
+//    lane holds 16 tokens' scores of its column.
+//  * PV, transposed (O^T = V^T P^T): A = V^T needs 8 tokens of one column per
+//    lane.  The codes are staged in LDS as they come, and the transposing read of
+//    4-bit elements hands lane i of a group of 16 the i-th column of 16 rows; the
+//    rows are given in the order of the lane's own scores, so one read per 16
+//    columns feeds two matrix operations.  A value's scale belongs to its token and its
+//    block of 32 columns, so it cannot be applied to operand pairs of two tokens:
+//    it multiplies the weight instead, P' = p 2^(s - 127), exact apart from the
+//    one rounding of p to bf16.  That makes P' differ between the column blocks --
+//    and a 16-column operand has columns to spare: with G query heads per kv-head,
+//    REP = min(D / 32, 16 / G) columns per head each carry another block, and of the
+//    16 result columns only the one with the slice's block is kept (at G = 8 and
+//    head_dim 128 two blocks share a column and P' is formed twice).
+// Weights are rounded to bf16 for the product (half a step, 2^-9 of each); their sum
+// is taken in fp32 before that rounding.
+// The step's own key and value take part as given, in bf16, and are stored in 4 bits.
+#pragma once
+
+#include "common.hpp"
+#include "decode_attn.hpp"
+#include "decode_attn_mfma.hpp"
+#include "kv4_ops.hpp"
+
+namespace baton {
+
+template <int D>
+struct Kv4Geo {
+  static constexpr int kKk = D / 32;                     // QK operations per 16 tokens
+  static constexpr int kDt = D / 16;                     // 16-column slices
+  static constexpr int kNb = D / 32;                     // scale blocks per token
+  static constexpr int kRowB = D / 2;                    // bytes of codes per token
+  static constexpr int kVlanes = kRowB / 16;             // lanes per V row
+  static constexpr int kVLoads = kVlanes;                // V loads per 64 tokens
+  static constexpr int kVTok = kWave / kVlanes;          // V rows per load
+  // Padded LDS row: 20 banks (12 at head_dim 64) put the 16 rows of a
+  // transposing read on disjoint banks.
+  static constexpr int kLdsRow = kRowB + 16;
+  static constexpr int kLdsV = 64 * kLdsRow;
+  static constexpr int kLdsS = kNb * 64 * 4;             // V scales as fp32 [block][token]
+};
+
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ i32x2_t read_tr4(const uint8_t* p) {
+  return __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+      (__attribute__((address_space(3))) i32x2_t*)(const_cast<uint8_t*>(p)));
+}
+
+// What one 64-token block needs from memory.
+template <int D>
+struct Kv4Block {
+  uint32_t k[4][D / 32];          // tile j: the lane's quarter of key row 16 j + l % 16
+  uint32_t ks[4];                 // its scale byte
+  u32x4 v[Kv4Geo<D>::kVLoads];    // V rows, 16 bytes per lane
+  uint32_t vs;                    // scales of token l
+};
+
+template <int D, int G, int NW>
+__global__ void __launch_bounds__(kWave * NW) __attribute__((amdgpu_waves_per_eu(2)))
+attn_kv4_kernel(const AttnArgs a) {
+  using Geo = Kv4Geo<D>;
+  constexpr int KK = Geo::kKk, DT = Geo::kDt, NB = Geo::kNb, VPT = D / 8, REC = D + 4;
+  constexpr int REP = NB < 16 / G ? NB : 16 / G;   // columns per query head
+  constexpr int NS = NB / REP;                     // blocks per column
+  __shared__ __attribute__((aligned(16))) uint8_t lds_v[NW][Geo::kLdsV];
+  __shared__ __attribute__((aligned(16))) float lds_s[NW][NB * 64];
+  __shared__ float sm_m[NW][G], sm_l[NW][G];
+  static_assert(G * D * 4 <= Geo::kLdsV, "merge area");
+  int32_t item, h;
+  const Item desc = work_unit(a, item, h);
+  const int tid = threadIdx.x;
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave;
+  const int g4 = lane / 16, c16 = lane % 16;
+  const int head = c16 / REP, hb = c16 % REP;      // this column's head (none from G on) and place
+  uint8_t* lds = lds_v[w];
+  float* ldss = lds_s[w];
+
+  const int4 it = desc.span;
+  const int4 rw = desc.row;
+  const int b = it.x;
+  const int32_t n = it.w;
+  const int64_t bt = (int64_t)b * a.tw;
+  uint32_t* outw = a.out + ((bt * a.n_kv_heads + h) * G) * (D / 2);
+  if (n < 0) {                       // free slot: zero output rows
+    for (int v = tid; v < G * VPT; v += NW * kWave) reinterpret_cast<u32x4*>(outw)[v] = u32x4{0, 0, 0, 0};
+    return;
+  }
+  int32_t t_begin, t_end;            // this wave's share of the item's tokens
+  wave_share<NW, 64>(it.y, it.z, w, t_begin, t_end);
+  const int64_t row = (int64_t)b * a.n_kv_heads + h;
+  const int64_t row_bytes = kv4_row_bytes(a.cap, D);
+  uint8_t* krow = reinterpret_cast<uint8_t*>(a.k_w) + row * row_bytes;
+  uint8_t* vrow = reinterpret_cast<uint8_t*>(a.v) + row * row_bytes;
+  const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(krow, 0, (uint32_t)row_bytes, kBufferWord3);
+  const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(vrow, 0, (uint32_t)row_bytes, kBufferWord3);
+  const uint32_t cap = (uint32_t)a.cap, plane = cap * Geo::kRowB;
+  const uint32_t start = (uint32_t)ring_add(a.base, a.L - n, a.cap);
+
+  // Query heads as the B operand in the keys' order of d.
+  bf16x8 qb[KK];
+  const u32x4* qrow = reinterpret_cast<const u32x4*>(a.q) + ((bt * a.n_kv_heads + h) * G) * VPT;
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk)
+    qb[kk] = as_bf16x8(head < G ? qrow[head * VPT + KK * g4 + kk] : u32x4{0, 0, 0, 0});
+
+  float m = -INFINITY, lsum = 0.f;
+  f32x4 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // Loads of the block of tokens tok(0) .. tok(63); a negative token has an
+  // offset beyond the buffer, which loads zeros without a memory access.
+  auto issue = [&](auto&& tok, Kv4Block<D>& x) {
+    auto col = [&](int32_t t) {
+      const uint32_t c = start + (uint32_t)t;
+      return c >= cap ? c - cap : c;
+    };
+    constexpr uint32_t kNone = 0x80000000u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int32_t t = tok(16 * j + c16);
+      const uint32_t c = col(t);
+      const uint32_t off = t >= 0 ? c * Geo::kRowB + g4 * (D / 8) : kNone;
+      if constexpr (D == 128) {
+        const u32x4 q = load16(rk, off);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) x.k[j][kk] = q[kk];
+      } else {
+        const auto q = __builtin_amdgcn_raw_buffer_load_b64(rk, off, 0, BATON_ATTN_NT ? 2 : 0);
+        x.k[j][0] = q[0];
+        x.k[j][1] = q[1];
+      }
+      x.ks[j] = __builtin_amdgcn_raw_buffer_load_b8(rk, t >= 0 ? plane + c * NB + (D == 128 ? g4 : g4 / 2) : kNone, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < Geo::kVLoads; ++u) {
+      const int32_t t = tok(u * Geo::kVTok + lane / Geo::kVlanes);
+      x.v[u] = load16(rv, t >= 0 ? col(t) * Geo::kRowB + (lane % Geo::kVlanes) * 16 : kNone);
+    }
+    const int32_t t = tok(lane);
+    const uint32_t off = t >= 0 ? plane + col(t) * NB : kNone;
+    if constexpr (D == 128) x.vs = __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0);
+    else x.vs = __builtin_amdgcn_raw_buffer_load_b16(rv, off, 0, 0);
+  };
+
+  // Scores, online softmax and PV of a block whose first nv tokens are valid.
+  auto block = [&](const Kv4Block<D>& x, int32_t nv) {
+#pragma unroll
+    for (int u = 0; u < Geo::kVLoads; ++u)
+      *reinterpret_cast<u32x4*>(lds + (u * Geo::kVTok + lane / Geo::kVlanes) * Geo::kLdsRow +
+                                (lane % Geo::kVlanes) * 16) = x.v[u];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) ldss[k * 64 + lane] = mx_scale_value((x.vs >> (8 * k)) & 255u);
+    float s[16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float sc = mx_scale_value(x.ks[j]);
+      f32x4 sj = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+        sj = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(mx_widen(x.k[j][kk], sc)), qb[kk], sj, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[4 * j + r] = sj[r] * a.qscale;
+    }
+    if (nv < 64) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (16 * (e / 4) + 4 * g4 + e % 4 >= nv) s[e] = -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    mx = fmaxf(m, max_over_groups(mx));
+    if (__builtin_amdgcn_ballot_w64(mx > m)) {    // some column's maximum rose
+      const float alpha = fast_exp2(m - mx);       // 0 from -inf; NaN where both are, mended below
+      const float f = m == -INFINITY ? 0.f : alpha;
+      lsum *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
+      m = mx;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    float p[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = fast_exp2(s[e] - ref);
+      lsum += p[e];
+    }
+    // P' operands: [set][half of the tokens]
+    bf16x8 pb[NS][2];
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 sc = *reinterpret_cast<const f32x4*>(ldss + (hb * NS + t) * 64 + 16 * j + 4 * g4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) pb[t][j / 2][4 * (j % 2) + r] = (__bf16)(p[4 * j + r] * sc[r]);
+      }
+    const uint8_t* vt = lds + (16 * (c16 / 4) + 4 * g4 + c16 % 4) * Geo::kLdsRow;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const i32x2_t c = read_tr4(vt + dt * 8);
+      const int t = (dt / 2) % NS;
+      o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(mx_widen(c[0], 1.f)), pb[t][0], o[dt], 0, 0, 0);
+      o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(mx_widen(c[1], 1.f)), pb[t][1], o[dt], 0, 0, 0);
+    }
+  };
+
+  const bool gathered = (rw.w & kGathered) != 0;
+  if (gathered) {
+    for (int32_t i0 = t_begin; i0 < t_end; i0 += 64) {
+      Kv4Block<D> x;
+      issue([&](int32_t i) { return i0 + i < t_end ? a.gather[i0 + i] : -1; }, x);
+      block(x, t_end - i0);
+    }
+  } else {
+    const int32_t c_end = min(t_end, n);
+    if (t_begin < c_end) {
+      Kv4Block<D> xa, xb;
+      auto tok = [&](int32_t tt) { return [tt, c_end](int32_t i) { return tt + i < c_end ? tt + i : -1; }; };
+      issue(tok(t_begin), xa);
+      for (int32_t tt = t_begin; tt < c_end; tt += 128) {
+        issue(tok(tt + 64), xb);
+        __builtin_amdgcn_sched_barrier(0);   // keep the loads ahead of the computation
+        block(xa, c_end - tt);
+        if (tt + 64 >= c_end) break;
+        issue(tok(tt + 128), xa);
+        __builtin_amdgcn_sched_barrier(0);
+        block(xb, c_end - tt - 64);
+      }
+    }
+  }
+
+  // The current token, from k_new / v_new in bf16: row 0 of a tile of its own.
+  // Its key and value are then quantised into the ring (of a gathered item, by
+  // its first wave): lane i < D / 8 has K's elements 8 i .., the next D / 8 lanes V's.
+  if (gathered ? (rw.w & kCurrent) != 0 && w == 0 : n >= t_begin && n < t_end) {
+    const u32x4* knew = reinterpret_cast<const u32x4*>(a.knew) + (bt * a.n_kv_heads + h) * VPT;
+    const u32x4* vnew = reinterpret_cast<const u32x4*>(a.vnew) + (bt * a.n_kv_heads + h) * VPT;
+    f32x4 sj = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const u32x4 kw = c16 == 0 ? knew[KK * g4 + kk] : u32x4{0, 0, 0, 0};
+      sj = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kw), qb[kk], sj, 0, 0, 0);
+    }
+    const float s = g4 == 0 ? sj[0] * a.qscale : -INFINITY;
+    const float mx = fmaxf(m, max_over_groups(s));
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    const float f = m == -INFINITY ? 0.f : fast_exp2(m - ref);
+    const float p = fast_exp2(s - ref);
+    lsum = lsum * f + p;
+    m = mx;
+    bf16x8 pa;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pa[e] = (__bf16)(e == 0 ? p : 0.f);
+    const uint16_t* v16 = reinterpret_cast<const uint16_t*>(vnew);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const u32x4 vw = {g4 == 0 ? (uint32_t)v16[16 * dt + c16] : 0u, 0u, 0u, 0u};
+      o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vw), pa, o[dt] * f, 0, 0, 0);
+    }
+    const bool is_v = lane >= VPT;
+    const int e = lane % VPT;
+    uint32_t scale;
+    const uint32_t code = mx_quantise(is_v ? vnew[e] : knew[e], scale);
+    const uint32_t col = (uint32_t)ring_add(start, n, a.cap);
+    if (lane < 2 * VPT) {
+      uint8_t* dst = is_v ? vrow : krow;
+      reinterpret_cast<uint32_t*>(dst + (int64_t)col * Geo::kRowB)[e] = code;
+      if (e % 4 == 0) dst[(int64_t)plane + (int64_t)col * NB + e / 4] = (uint8_t)scale;
+    }
+  }
+
+  // A column keeps the slices of its own blocks: lane l's o[dt][r] is column
+  // 16 dt + 4 (l / 16) + r of its head.
+  lsum = sum_over_groups(lsum);
+  __builtin_amdgcn_wave_barrier();
+  if (head < G) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      if (dt / 2 / NS == hb) *reinterpret_cast<f32x4*>(lds + (head * D + 16 * dt + 4 * g4) * 4) = o[dt];
+    if (hb == 0 && g4 == 0) {
+      sm_m[w][head] = m;
+      sm_l[w][head] = lsum;
+    }
+  }
+  __syncthreads();
+  float* rec0 = a.partial + (((int64_t)h * a.n_items + item) * G) * REC;
+  wg_merge_write<BF16Tag, D, G, NW>(sm_m, sm_l, reinterpret_cast<const float*>(&lds_v[0][0]), Geo::kLdsV / 4,
+                                    rw.y == 1, outw, rec0, tid);
+}
+
+}  // namespace baton

@@ -97,8 +97,8 @@ class BatchScaler:
         import torch
         n = self.cache.tokens()[b]
         shape = (self.cache.n_layers, self.cache.n_kv_heads, n, self.cache.head_dim)
-        hk = torch.empty(shape, dtype=self.cache.k.dtype, pin_memory=True)
-        hv = torch.empty(shape, dtype=self.cache.k.dtype, pin_memory=True)
+        hk = torch.empty(shape, dtype=self.cache.io_dtype, pin_memory=True)
+        hv = torch.empty(shape, dtype=self.cache.io_dtype, pin_memory=True)
         B.baton_kv_extract(self.cache.handle, [b], [device_pointer(hk)], [device_pointer(hv)],
                            torch.cuda.current_stream())
         return {"k": hk, "v": hv, "n": n, "dk": None, "dv": None, "ready": None}
