@@ -500,6 +500,82 @@ baton_status baton_rope_qkv(const baton_cache* cache, const void* qkv, void* q, 
 baton_status baton_silu_mul(int32_t dtype, const void* gate_up, void* out, int32_t rows, int32_t dim,
                             hipStream_t stream);
 
+/*
+ * ---- What each query of a batch brings of its own -------------------------
+ *
+ * Low-rank adapters of many requests beside a shared projection: for every row
+ * r with adapter i = row_adapter[r],
+ *     y[r] (+)= scale_i * (x[r] . A_i^T) . B_i^T,
+ * accumulate = 1 adding to y (what baton_linear_packed left there), 0
+ * overwriting it.  row_adapter: host array of rows entries, each an index into
+ * adapters (host array of n_adapters; only those named by a row are read) or
+ * -1 for none: such a row is zeros (accumulate = 0) or left as it is (1).
+ * Projections fused along their outputs (query, key and value; gate and up)
+ * have an adapter for each part: the output's columns are n_parts ranges of
+ * part_dims[p] (host array; NULL with one part: all of out_dim), A_i holds
+ * n_parts * rank rows, and part p uses rows p * rank .. of it:
+ *     a: device [n_parts * rank][in_dim], b: device [out_dim][rank].
+ * x: device [rows <= BATON_GEMM_MAX_ROWS][in_dim], y: device [rows][out_dim];
+ * bf16, 16-byte aligned, y apart from everything read.  Ranks may differ
+ * between adapters (multiples of 8 up to BATON_ADAPTER_MAX_RANK; a smaller one
+ * is padded with zero rows of A and columns of B).  Products and sums are in
+ * fp32 (x . A^T is kept to 16 bits), in a fixed order, and y is rounded once.
+ * ws: device workspace of at least baton_linear_adapters_workspace_bytes(rows,
+ * n_parts, the largest rank a row uses), 16-byte aligned; a multiple of that
+ * lets in_dim be divided over more workgroups.  Calls that share a workspace go
+ * to one stream.  Nothing is read or written when no row has an adapter and
+ * accumulate = 1.
+ * Errors: EINVAL (null or misaligned pointer, rows outside
+ * 1..BATON_GEMM_MAX_ROWS, sizes not positive multiples of 8, part_dims that do
+ * not add up to out_dim, n_parts outside 1..BATON_ADAPTER_MAX_PARTS, an adapter
+ * out of range, its rank or scale unsupported, accumulate not 0/1, ws too
+ * small), EDTYPE (not bf16), EHIP.
+ */
+#define BATON_ADAPTER_MAX_RANK 128
+#define BATON_ADAPTER_MAX_PARTS 4
+
+typedef struct baton_adapter {
+  const void* a; /* device, [n_parts * rank][in_dim] */
+  const void* b; /* device, [out_dim][rank] */
+  int32_t rank;
+  float scale;
+} baton_adapter;
+
+size_t baton_linear_adapters_workspace_bytes(int32_t rows, int32_t n_parts, int32_t max_rank);
+baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_adapter* adapters, int32_t n_adapters,
+                                   const int32_t* row_adapter, void* y, int32_t rows, int32_t out_dim,
+                                   int32_t in_dim, const int32_t* part_dims, int32_t n_parts, int32_t accumulate,
+                                   void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * One token per row of logits (device [rows] of vocab elements, fp32 or bf16,
+ * ld elements from row to row), each row with its own parameters and its own
+ * uniform random number u[r].  All parameters are device arrays of rows
+ * entries, so a captured call follows them; NULL stands for the value that
+ * changes nothing.  With w_i = exp((l_i - max l) / temperature) and the tokens
+ * ordered by (logit descending, index ascending), the kept tokens are the
+ * shortest of
+ *   - the first top_k of them (top_k <= 0 or >= vocab: all),
+ *   - the fewest first ones whose weight is at least top_p times the weight of
+ *     the first top_k (top_p >= 1 or NaN: all; <= 0: one),
+ *   - those with w_i >= min_p (min_p <= 0 or NaN: all; the first one always),
+ * and tokens[r] is the first kept token, in order of index, at which the
+ * running weight of the kept tokens exceeds u times all of it (u is taken into
+ * [0, 1), a NaN as 0).  A temperature that is not positive (or NaN) takes the
+ * first token of the order; so do top_k = 1 and min_p > 1.
+ * A logit that is NaN or -inf is never drawn; a row of nothing else gives -1.
+ * +inf is above every number: beside it only other infinities are drawn,
+ * alike.  Weights and their sums have 38 bits or more behind the binary point
+ * (45 at a vocabulary of 128,000), sums in any order alike, so the same inputs
+ * give the same token.
+ * logits aligned to their element; the arrays to 4 bytes.
+ * Errors: EINVAL (null logits, u or tokens, rows < 1, vocab outside 1..2^24,
+ * ld < vocab, misaligned pointer), EDTYPE, EHIP.
+ */
+baton_status baton_sample(int32_t dtype, const void* logits, int64_t ld, int32_t rows, int32_t vocab,
+                          const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                          const float* u, int32_t* tokens, hipStream_t stream);
+
 /* Static English text of a status. */
 const char* baton_status_string(baton_status status);
 

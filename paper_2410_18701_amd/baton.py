@@ -18,6 +18,8 @@ STATUS_NAMES = ["BATON_OK", "BATON_EINVAL", "BATON_ESLOT", "BATON_ECAPACITY", "B
                 "BATON_ESTATE", "BATON_EHIP", "BATON_ESCRATCH"]
 BATON_SCRATCH_BYTES = 64 << 20
 BATON_GEMM_MAX_ROWS = 256
+BATON_ADAPTER_MAX_RANK = 128
+BATON_ADAPTER_MAX_PARTS = 4
 BATON_F32, BATON_BF16, BATON_MXFP4 = 0, 1, 2
 BATON_FILL_NEG_INF_F32 = 0xFF800000
 BATON_FILL_NEG_INF_BF16 = 0xFF80
@@ -36,6 +38,11 @@ class baton_cache_desc(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("capacity", ctypes.c_int64),
                 ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("fill_bits", ctypes.c_uint32),
                 ("layer_stride", ctypes.c_int64)]
+
+
+class baton_adapter(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("rank", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 class BatonError(RuntimeError):
@@ -85,6 +92,11 @@ def lib():
         L.baton_rmsnorm.argtypes = [i32, vp, vp, vp, i32, i32, ctypes.c_float, vp]
         L.baton_rope_qkv.argtypes = [vp, vp, vp, vp, vp, ctypes.c_float, vp]
         L.baton_silu_mul.argtypes = [i32, vp, vp, i32, i32, vp]
+        L.baton_linear_adapters_workspace_bytes.argtypes = [i32, i32, i32]
+        L.baton_linear_adapters_workspace_bytes.restype = ctypes.c_size_t
+        L.baton_linear_adapters.argtypes = [i32, vp, P(baton_adapter), i32, P(i32), vp, i32, i32, i32, P(i32), i32,
+                                            i32, vp, ctypes.c_size_t, vp]
+        L.baton_sample.argtypes = [i32, vp, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp]
         L.baton_status_string.argtypes = [st]
         L.baton_status_string.restype = ctypes.c_char_p
         for name in ("baton_cache_create", "baton_cache_destroy", "baton_kv_evict", "baton_kv_embed",
@@ -93,7 +105,7 @@ def lib():
                      "baton_cache_query", "baton_set_split_tokens", "baton_cache_flush",
                      "baton_shape_insert", "baton_cache_tokens", "baton_kv_move", "baton_linear_pack", "baton_linear_packed",
                      "baton_linear_packed_rmsnorm", "baton_linear_packed_silu",
-                     "baton_rmsnorm", "baton_rope_qkv", "baton_silu_mul"):
+                     "baton_rmsnorm", "baton_rope_qkv", "baton_silu_mul", "baton_linear_adapters", "baton_sample"):
             getattr(L, name).restype = st
         _lib = L
     return _lib
@@ -275,3 +287,26 @@ def baton_rope_qkv(cache, qkv, q, k_new, v_new, theta, stream=None):
 
 def baton_silu_mul(dtype, gate_up, out, rows, dim, stream=None):
     _check(lib().baton_silu_mul(dtype, _ptr(gate_up), _ptr(out), rows, dim, _stream(stream)), "baton_silu_mul")
+
+
+# ---- what each query brings of its own ----
+def baton_linear_adapters_workspace_bytes(rows, n_parts, max_rank):
+    return lib().baton_linear_adapters_workspace_bytes(rows, n_parts, max_rank)
+
+
+def baton_linear_adapters(dtype, x, adapters, n_adapters, row_adapter, y, rows, out_dim, in_dim, part_dims, n_parts,
+                          accumulate, ws, ws_bytes, stream=None):
+    """adapters: a ctypes array of baton_adapter (or None); row_adapter: rows integers;
+    part_dims: n_parts integers or None."""
+    ids = (ctypes.c_int32 * max(1, len(row_adapter)))(*row_adapter)
+    if len(row_adapter) != rows or (part_dims is not None and len(part_dims) != n_parts):
+        raise ValueError("row_adapter needs an entry per row, part_dims one per part")
+    parts = None if part_dims is None else (ctypes.c_int32 * max(1, n_parts))(*part_dims)
+    _check(lib().baton_linear_adapters(dtype, _ptr(x), adapters, n_adapters, ids, _ptr(y), rows, out_dim, in_dim,
+                                       parts, n_parts, int(accumulate), _ptr(ws), ws_bytes, _stream(stream)),
+           "baton_linear_adapters")
+
+
+def baton_sample(dtype, logits, ld, rows, vocab, temperature, top_k, top_p, min_p, u, tokens, stream=None):
+    _check(lib().baton_sample(dtype, _ptr(logits), ld, rows, vocab, _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                              _ptr(min_p), _ptr(u), _ptr(tokens), _stream(stream)), "baton_sample")

@@ -5,7 +5,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libbaton.so")
-SOURCES = [os.path.join(HERE, "csrc", "baton.hip"), os.path.join(HERE, "csrc", "layer.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("baton.hip", "layer.hip", "adapters.hip", "sample.hip")]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",

@@ -1,0 +1,225 @@
+// Low-rank adapters of many requests beside a shared projection:
+//   y[r] (+)= scale_g * (x[r] . A_g^T) . B_g^T,  g the adapter of row r,
+// in two launches over the rows sorted by adapter.  What bounds both is reading
+// the adapters' weights once (and, for a few small ones, the launches' latency):
+// a batch of 64 rows over 24 adapters does 1 to 3 flops per byte.
+//  * down: h = x . A^T, [rows][parts * rank].  A workgroup takes 16 of an
+//    adapter's rows of A, up to 64 of its batch rows and a range of k; its four
+//    waves divide the range and add through LDS.  Ranges are taken so that
+//    the launch has a few waves per SIMD whatever the number of adapters; each
+//    range's sums go to the workspace in fp32.
+//  * up: the ranges' sums are added in order, scaled, and split into two bf16
+//    halves (the value and what its rounding leaves: 16 bits of it), staged in LDS;
+//    then 16 x 16 tiles of y = h . B^T, every wave its own columns.  The second half
+//    costs one more matrix operation on operands that are in registers; without it
+//    h would be rounded to 8 bits.
+// Sums are fp32 in a fixed order: the same call gives the same bits.
+#pragma once
+
+#include <type_traits>
+
+#include "common.hpp"
+
+namespace baton {
+namespace {
+
+typedef __bf16 ad_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float ad_f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kAdapterWaves = 4;
+constexpr int kAdapterRows = 64;      // batch rows a workgroup takes at most
+constexpr int kAdapterMaxRank = 128;  // == BATON_ADAPTER_MAX_RANK
+constexpr int kAdapterGroups = 96;    // adapters per launch (the arguments are 4 KB at most)
+constexpr int kAdapterMaxRows = 256;  // == BATON_GEMM_MAX_ROWS
+
+// The rows of one adapter: places [begin, next group's begin) of the sorted rows.
+struct AdapterGroup {
+  const uint16_t* a;    // [parts * rank][K]; null: rows without an adapter
+  const uint16_t* b;    // [N][rank]
+  float scale;
+  int16_t rank, begin;
+  int32_t down_end, up_end;   // workgroups up to this group's last one, of each launch
+};
+
+struct AdapterArgs {
+  const uint16_t* x;    // [rows][K]
+  uint16_t* y;          // [rows][N]
+  float* h;             // [splits][rows][hs]
+  int32_t K, N, rows, hs, parts, splits, n_groups, accumulate;
+  int32_t kt;           // 32-wide steps of k per split
+  int32_t cols;         // columns of y per wave, a multiple of 32
+  int32_t part_end[4];  // columns of y up to the end of each part
+  AdapterGroup g[kAdapterGroups];
+  int16_t end;          // sorted rows of this launch end here
+  uint16_t row[kAdapterMaxRows];   // sorted place -> batch row
+};
+static_assert(sizeof(AdapterArgs) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ ad_bf16x8 ad_vec(const u32x4& w) { return __builtin_bit_cast(ad_bf16x8, w); }
+
+// The group of workgroup i of a launch.
+template <bool UP>
+__device__ __forceinline__ int adapter_group(const AdapterArgs& a, int32_t i) {
+  int lo = 0, hi = a.n_groups - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (i < (UP ? a.g[mid].up_end : a.g[mid].down_end)) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+__global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_down_kernel(const AdapterArgs a) {
+  __shared__ ad_f32x4 part[kAdapterWaves][kAdapterRows / 16][kWave];
+  const int gi = adapter_group<false>(a, blockIdx.x);
+  const AdapterGroup& g = a.g[gi];
+  const int local = (int)blockIdx.x - (gi > 0 ? a.g[gi - 1].down_end : 0);
+  const int n_r = a.parts * g.rank, tiles = (n_r + 15) / 16;
+  const int tile = local % tiles, rest = local / tiles, split = rest % a.splits, rb = rest / a.splits;
+  const int first = g.begin + rb * kAdapterRows;
+  const int n = min((gi + 1 < a.n_groups ? a.g[gi + 1].begin : a.end) - first, kAdapterRows);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int g4 = lane / 16, c16 = lane % 16;
+  const int n_rt = (n + 15) / 16;      // tiles of batch rows
+  // this wave's steps of k
+  const int per = (a.kt + kAdapterWaves - 1) / kAdapterWaves;
+  const int s0 = split * a.kt + w * per, s1 = min(min(s0 + per, (split + 1) * a.kt), (a.K + 31) / 32);
+  // rows past the last one read it again; their sums are not stored
+  const uint16_t* ar = g.a + (int64_t)min(tile * 16 + c16, n_r - 1) * a.K + 8 * g4;
+  const uint16_t* xr[kAdapterRows / 16];
+#pragma unroll
+  for (int t = 0; t < kAdapterRows / 16; ++t)
+    xr[t] = a.x + (int64_t)a.row[first + min(16 * t + c16, n - 1)] * a.K + 8 * g4;
+  ad_f32x4 acc[kAdapterRows / 16];
+#pragma unroll
+  for (int t = 0; t < kAdapterRows / 16; ++t) acc[t] = ad_f32x4{0.f, 0.f, 0.f, 0.f};
+  const u32x4 zero = {0, 0, 0, 0};
+  auto run = [&](auto nt_tag) {
+    constexpr int NT = decltype(nt_tag)::value, U = NT == 1 ? 8 : NT == 2 ? 4 : 2;   // U steps' loads in flight
+    for (int s = s0; s < s1; s += U) {
+      u32x4 aw[U], xw[U][NT];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int k = 32 * (s + i);
+        const bool in = s + i < s1 && k + 8 * g4 < a.K;   // K is a multiple of 8
+        aw[i] = in ? *reinterpret_cast<const u32x4*>(ar + k) : zero;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) xw[i][t] = in ? *reinterpret_cast<const u32x4*>(xr[t] + k) : zero;
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(aw[i]), ad_vec(xw[i][t]), acc[t], 0, 0, 0);
+    }
+  };
+  if (n_rt == 1) run(std::integral_constant<int, 1>{});
+  else if (n_rt == 2) run(std::integral_constant<int, 2>{});
+  else run(std::integral_constant<int, 4>{});
+#pragma unroll
+  for (int t = 0; t < kAdapterRows / 16; ++t)
+    if (t < n_rt) part[w][t][lane] = acc[t];
+  __syncthreads();
+  // wave t adds tile t's sums: lane l has rows 4 (l / 16) .. + 3 of A for batch row l % 16
+  if (w >= n_rt) return;
+  ad_f32x4 sum = part[0][w][lane];
+#pragma unroll
+  for (int v = 1; v < kAdapterWaves; ++v) sum += part[v][w][lane];
+  const int r = 16 * w + c16, j = tile * 16 + 4 * g4;
+  if (r < n && j < n_r)     // n_r is a multiple of 8
+    *reinterpret_cast<ad_f32x4*>(a.h + ((int64_t)split * a.rows + first + r) * a.hs + j) = sum;
+}
+
+__global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const AdapterArgs a) {
+  constexpr int ROW = kAdapterMaxRank + 8;     // bf16 elements per staged row, padded
+  __shared__ __attribute__((aligned(16))) uint16_t hs_hi[kAdapterRows * ROW], hs_lo[kAdapterRows * ROW];
+  const int gi = adapter_group<true>(a, blockIdx.x);
+  const AdapterGroup& g = a.g[gi];
+  const int local = (int)blockIdx.x - (gi > 0 ? a.g[gi - 1].up_end : 0);
+  // the workgroup's columns: part by part, kAdapterWaves * cols at a time
+  int per_rb = 0, p = 0, c0 = 0, c_end = 0;
+  const int wide = kAdapterWaves * a.cols;
+  for (int q = 0; q < a.parts; ++q) per_rb += (a.part_end[q] - (q > 0 ? a.part_end[q - 1] : 0) + wide - 1) / wide;
+  const int rb = local / per_rb;
+  int chunk = local - rb * per_rb;
+  for (int q = 0; q < a.parts; ++q) {
+    const int b0 = q > 0 ? a.part_end[q - 1] : 0, cnt = (a.part_end[q] - b0 + wide - 1) / wide;
+    if (chunk < cnt) {
+      p = q;
+      c0 = b0 + chunk * wide;
+      c_end = a.part_end[q];
+      break;
+    }
+    chunk -= cnt;
+  }
+  const int first = g.begin + rb * kAdapterRows;
+  const int n = min((gi + 1 < a.n_groups ? a.g[gi + 1].begin : a.end) - first, kAdapterRows);
+  const int rank = g.rank, n_kk = (rank + 31) / 32, n_rt = (n + 15) / 16;
+  const int tid = threadIdx.x, lane = tid % kWave, g4 = lane / 16, c16 = lane % 16;
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  // h of the part, four elements per thread and step; zeros up to whole operands
+  const int quads = n_kk * 8;
+  for (int i = tid; i < n_rt * 16 * quads; i += kWave * kAdapterWaves) {
+    const int r = i / quads, j = 4 * (i % quads);
+    ad_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (r < n && j < rank) {
+      const float* src = a.h + (int64_t)(first + r) * a.hs + p * rank + j;
+      for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const ad_f32x4*>(src + (int64_t)s * a.rows * a.hs);
+    }
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float f = v[e] * g.scale;
+      hi[e] = f32_to_bf16_rne(f);
+      // nothing remains of what rounds to an infinity (or is one, or a NaN)
+      lo[e] = (hi[e] & 0x7F80u) == 0x7F80u ? 0u : f32_to_bf16_rne(f - __uint_as_float(hi[e] << 16));
+    }
+    *reinterpret_cast<uint2*>(hs_hi + r * ROW + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+    *reinterpret_cast<uint2*>(hs_lo + r * ROW + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+  }
+  __syncthreads();
+  const u32x4 zero = {0, 0, 0, 0};
+  const int w0 = c0 + w * a.cols, w1 = min(w0 + a.cols, c_end);
+  // 32 columns at a time: row 4 g + r of tile j is column 8 g + 4 j + r, so a lane
+  // ends with 8 neighbouring columns of its batch row
+  for (int c = w0; c < w1; c += 32) {
+    ad_bf16x8 bv[2][kAdapterMaxRank / 32];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int col = c + 8 * (c16 / 4) + 4 * j + c16 % 4;
+      const uint16_t* br = g.b + (int64_t)min(col, c_end - 1) * rank + 8 * g4;
+#pragma unroll
+      for (int kk = 0; kk < kAdapterMaxRank / 32; ++kk)
+        if (kk < n_kk)
+          bv[j][kk] = ad_vec(32 * kk + 8 * g4 < rank ? *reinterpret_cast<const u32x4*>(br + 32 * kk) : zero);
+    }
+    for (int t = 0; t < n_rt; ++t) {
+      const int r = 16 * t + c16;
+      const bool ok = r < n && c + 8 * g4 < w1;     // w1 is a multiple of 8
+      u32x4* yp = reinterpret_cast<u32x4*>(a.y + (int64_t)a.row[first + min(r, n - 1)] * a.N + c + 8 * g4);
+      u32x4 old = zero;
+      if (ok && a.accumulate) old = *yp;
+      ad_f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int kk = 0; kk < kAdapterMaxRank / 32; ++kk)
+        if (kk < n_kk) {
+          const ad_bf16x8 hi = ad_vec(*reinterpret_cast<const u32x4*>(hs_hi + r * ROW + 32 * kk + 8 * g4));
+          const ad_bf16x8 lo = ad_vec(*reinterpret_cast<const u32x4*>(hs_lo + r * ROW + 32 * kk + 8 * g4));
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[j][kk], lo, acc[j], 0, 0, 0);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[j][kk], hi, acc[j], 0, 0, 0);
+          }
+        }
+      u32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        o[e] = f32_to_bf16_rne(bf16_lo(old[e]) + acc[e / 2][2 * (e % 2)]) |
+               f32_to_bf16_rne(bf16_hi(old[e]) + acc[e / 2][2 * (e % 2) + 1]) << 16;
+      if (ok) *yp = o;
+    }
+  }
+}
+
+}  // namespace
+}  // namespace baton

@@ -18,6 +18,35 @@ class PackedWeight:
         self.data, self.out_dim, self.in_dim = data, out_dim, in_dim
 
 
+class Adapters:
+    """Low-rank adapters of one projection: a[i] [parts * rank_i][in], b[i] [out][rank_i]
+    bf16 tensors, scales[i]; parts: the widths of the output's parts when the projection
+    is fused along its outputs (query, key and value; gate and up), each with rows of a
+    of its own.  The tensors are used in place."""
+
+    def __init__(self, a, b, scales, parts=None):
+        import torch
+        if not len(a) == len(b) == len(scales):
+            raise ValueError("Adapters: a, b and scales need the same length")
+        self.a, self.b, self.n = list(a), list(b), len(a)
+        self.parts = None if parts is None else [int(p) for p in parts]
+        n_parts = 1 if parts is None else len(self.parts)
+        self.max_rank = max((t.shape[1] for t in self.b), default=0)
+        self.table = (B.baton_adapter * max(1, self.n))()
+        for i, (ai, bi, s) in enumerate(zip(self.a, self.b, scales)):
+            if ai.shape[0] != n_parts * bi.shape[1] or ai.shape[1] != self.a[0].shape[1] or \
+                    bi.shape[0] != self.b[0].shape[0]:
+                raise ValueError(f"Adapters: shapes of adapter {i} do not match")
+            for t in (ai, bi):
+                if t.dtype != torch.bfloat16 or not t.is_contiguous():
+                    raise ValueError("Adapters: contiguous bf16 tensors only")
+            self.table[i] = B.baton_adapter(ai.data_ptr(), bi.data_ptr(), bi.shape[1], float(s))
+        self.in_dim = self.a[0].shape[1] if self.n else None
+        self.out_dim = self.b[0].shape[0] if self.n else None
+        if self.n and parts is not None and sum(self.parts) != self.out_dim:
+            raise ValueError("Adapters: parts do not add up to the output")
+
+
 class Gemm:
     """The device workspace of the projections (the partial sums of
     baton_linear_packed when it splits along in_dim), and the projection calls."""
@@ -75,6 +104,21 @@ class Gemm:
                                       eps, y_norm, self.ws, self.ws_bytes, _stream())
         return y
 
+    def linear_adapters(self, x, adapters, row_adapter, y, accumulate=False):
+        """y (+)= each row's low-rank product with its adapter: x [rows <= 256][in], y [rows][out],
+        row_adapter a list of rows indices into adapters (-1: none)."""
+        rows, in_dim = x.shape
+        if y.shape[0] != rows or y.dim() != 2 or len(row_adapter) != rows or \
+                (adapters.n and (in_dim != adapters.in_dim or y.shape[1] != adapters.out_dim)):
+            raise ValueError("linear_adapters: shapes do not match")
+        for t in (x, y):
+            if not t.is_contiguous():
+                raise ValueError("linear_adapters: contiguous tensors only")
+        B.baton_linear_adapters(B.BATON_BF16, x, adapters.table, adapters.n, row_adapter, y, rows, y.shape[1], in_dim,
+                                adapters.parts, 1 if adapters.parts is None else len(adapters.parts), accumulate,
+                                self.ws, self.ws_bytes, _stream())
+        return y
+
     def close(self):
         self.ws = None
 
@@ -103,6 +147,37 @@ def rope_qkv(cache, qkv, q, k_new, v_new, theta):
             k_new.numel() != cache.batch * cache.n_kv_heads * cache.head_dim or v_new.numel() != k_new.numel():
         raise ValueError("rope_qkv: output sizes do not match the cache")
     B.baton_rope_qkv(cache.handle, qkv, q, k_new, v_new, theta, _stream())
+
+
+class Sampler:
+    """One token per row of logits, with each row's own parameters (device tensors of
+    rows entries, or None) and uniform random numbers u.  The tokens, int32 [rows],
+    are written to the same tensor by every call."""
+
+    def __init__(self, rows, vocab):
+        import torch
+        self.rows, self.vocab = rows, vocab
+        self.tokens = torch.empty(rows, dtype=torch.int32, device="cuda")
+
+    def __call__(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
+        """logits [rows][vocab], fp32 or bf16, rows any distance apart."""
+        import torch
+        if tuple(logits.shape) != (self.rows, self.vocab) or (self.vocab > 1 and logits.stride(1) != 1):
+            raise ValueError("Sampler: logits must be [rows][vocab], each row dense")
+        dtype = {torch.float32: B.BATON_F32, torch.bfloat16: B.BATON_BF16}.get(logits.dtype)
+        if dtype is None:
+            raise ValueError("Sampler: fp32 or bf16 logits")
+        for name, t, want in (("u", u, torch.float32), ("temperature", temperature, torch.float32),
+                              ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                              ("min_p", min_p, torch.float32)):
+            if t is None and name != "u":
+                continue
+            if t.dtype != want or t.numel() != self.rows or not t.is_contiguous():
+                raise ValueError(f"Sampler: {name} must be {self.rows} contiguous {want} values")
+        ld = logits.stride(0) if self.rows > 1 else self.vocab
+        B.baton_sample(dtype, logits, ld, self.rows, self.vocab, temperature, top_k, top_p, min_p, u, self.tokens,
+                       _stream())
+        return self.tokens
 
 
 class DecodeLayers:
