@@ -338,7 +338,7 @@ void plan_items(baton_cache* c, baton::MetaArgs& m, int64_t& items, int64_t& mul
   std::memset(&m, 0, sizeof(m));
   m.L = c->L;
   m.batch = c->d.batch;
-  c->step_split = c->split > 0 ? c->split : auto_split(c);
+  c->step_split = c->split > 0 ? c->split : is_kv4(c) ? kv4_split(c) : auto_split(c);
   m.split = c->step_split;
   m.gather_max = gather_max(c);
   m.holes = hole_list(c);

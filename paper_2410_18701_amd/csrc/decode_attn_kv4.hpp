@@ -31,6 +31,10 @@
 // The step's own key and value take part as given, in bf16, and are stored in 4 bits.
 #pragma once
 
+#ifndef BATON_KV4_WPE
+#define BATON_KV4_WPE 3
+#endif
+
 #include "common.hpp"
 #include "decode_attn.hpp"
 #include "decode_attn_mfma.hpp"
@@ -71,7 +75,7 @@ struct Kv4Block {
 };
 
 template <int D, int G, int NW>
-__global__ void __launch_bounds__(kWave * NW) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ void __launch_bounds__(kWave * NW) __attribute__((amdgpu_waves_per_eu(BATON_KV4_WPE)))
 attn_kv4_kernel(const AttnArgs a) {
   using Geo = Kv4Geo<D>;
   constexpr int KK = Geo::kKk, DT = Geo::kDt, NB = Geo::kNb, VPT = D / 8, REC = D + 4;
@@ -100,8 +104,7 @@ attn_kv4_kernel(const AttnArgs a) {
     for (int v = tid; v < G * VPT; v += NW * kWave) reinterpret_cast<u32x4*>(outw)[v] = u32x4{0, 0, 0, 0};
     return;
   }
-  int32_t t_begin, t_end;            // this wave's share of the item's tokens
-  wave_share<NW, 64>(it.y, it.z, w, t_begin, t_end);
+  const int32_t t_begin = it.y, t_end = it.z;
   const int64_t row = (int64_t)b * a.n_kv_heads + h;
   const int64_t row_bytes = kv4_row_bytes(a.cap, D);
   uint8_t* krow = reinterpret_cast<uint8_t*>(a.k_w) + row * row_bytes;
@@ -111,51 +114,77 @@ attn_kv4_kernel(const AttnArgs a) {
   const uint32_t cap = (uint32_t)a.cap, plane = cap * Geo::kRowB;
   const uint32_t start = (uint32_t)ring_add(a.base, a.L - n, a.cap);
 
-  // Query heads as the B operand in the keys' order of d.
+  auto load_k = [&](uint32_t off, uint32_t (&k)[KK]) {
+    if constexpr (D == 128) {
+      const u32x4 q = load16(rk, off);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) k[kk] = q[kk];
+    } else {
+      const auto q = __builtin_amdgcn_raw_buffer_load_b64(rk, off, 0, BATON_ATTN_NT ? 2 : 0);
+      k[0] = q[0];
+      k[1] = q[1];
+    }
+  };
+  auto load_vs = [&](uint32_t off) -> uint32_t {
+    if constexpr (D == 128) return __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b16(rv, off, 0, 0);
+  };
+
+  // Query heads as the B operand in the keys' order of d, negated for a negative
+  // scale, so that the largest score is the largest product.
+  const float qs = fabsf(a.qscale);
+  const uint32_t flip = a.qscale < 0.f ? 0x80008000u : 0u;
   bf16x8 qb[KK];
   const u32x4* qrow = reinterpret_cast<const u32x4*>(a.q) + ((bt * a.n_kv_heads + h) * G) * VPT;
 #pragma unroll
-  for (int kk = 0; kk < KK; ++kk)
-    qb[kk] = as_bf16x8(head < G ? qrow[head * VPT + KK * g4 + kk] : u32x4{0, 0, 0, 0});
+  for (int kk = 0; kk < KK; ++kk) {
+    const u32x4 qw = head < G ? qrow[head * VPT + KK * g4 + kk] : u32x4{0, 0, 0, 0};
+    qb[kk] = as_bf16x8(qw ^ flip);
+  }
 
   float m = -INFINITY, lsum = 0.f;
   f32x4 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // Loads of the block of tokens tok(0) .. tok(63); a negative token has an
-  // offset beyond the buffer, which loads zeros without a memory access.
-  auto issue = [&](auto&& tok, Kv4Block<D>& x) {
-    auto col = [&](int32_t t) {
-      const uint32_t c = start + (uint32_t)t;
-      return c >= cap ? c - cap : c;
-    };
-    constexpr uint32_t kNone = 0x80000000u;
+  // Loads of 64 consecutive columns of the ring from col on.  Those past the row's
+  // last column find other bytes of the row or, past its end, zeros.
+  const uint32_t k_lane = c16 * Geo::kRowB + g4 * (D / 8), ks_lane = c16 * NB + (D == 128 ? g4 : g4 / 2);
+  // Not live: beyond the buffer, which loads zeros without an access.
+  constexpr uint32_t kNone = 0x80000000u;
+  auto issue = [&](bool live, uint32_t col, Kv4Block<D>& x) {
+    const uint32_t cb = live ? col * Geo::kRowB : kNone, sb = live ? plane + col * NB : kNone;
+    const uint32_t ko = cb + k_lane, so = sb + ks_lane;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int32_t t = tok(16 * j + c16);
-      const uint32_t c = col(t);
-      const uint32_t off = t >= 0 ? c * Geo::kRowB + g4 * (D / 8) : kNone;
-      if constexpr (D == 128) {
-        const u32x4 q = load16(rk, off);
+      load_k(ko + j * 16 * Geo::kRowB, x.k[j]);
+      x.ks[j] = __builtin_amdgcn_raw_buffer_load_b8(rk, so + j * 16 * NB, 0, 0);
+    }
+    const uint32_t vo = cb + lane * 16;
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) x.k[j][kk] = q[kk];
-      } else {
-        const auto q = __builtin_amdgcn_raw_buffer_load_b64(rk, off, 0, BATON_ATTN_NT ? 2 : 0);
-        x.k[j][0] = q[0];
-        x.k[j][1] = q[1];
-      }
-      x.ks[j] = __builtin_amdgcn_raw_buffer_load_b8(rk, t >= 0 ? plane + c * NB + (D == 128 ? g4 : g4 / 2) : kNone, 0, 0);
+    for (int u = 0; u < Geo::kVLoads; ++u) x.v[u] = load16(rv, vo + u * 1024);
+    x.vs = load_vs(sb + lane * NB);
+  };
+  // The same for the tokens of a gather list, from place i0 on; none past its end.
+  auto issue_listed = [&](int32_t i0, int32_t i1, Kv4Block<D>& x) {
+    auto col = [&](int32_t i) {   // its ring column, or cap
+      if (i >= i1) return cap;
+      const uint32_t c = start + (uint32_t)a.gather[i];
+      return c >= cap ? c - cap : c;
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t c = col(i0 + 16 * j + c16);
+      load_k(c < cap ? c * Geo::kRowB + g4 * (D / 8) : kNone, x.k[j]);
+      x.ks[j] = __builtin_amdgcn_raw_buffer_load_b8(rk, c < cap ? plane + c * NB + (D == 128 ? g4 : g4 / 2) : kNone, 0, 0);
     }
 #pragma unroll
     for (int u = 0; u < Geo::kVLoads; ++u) {
-      const int32_t t = tok(u * Geo::kVTok + lane / Geo::kVlanes);
-      x.v[u] = load16(rv, t >= 0 ? col(t) * Geo::kRowB + (lane % Geo::kVlanes) * 16 : kNone);
+      const uint32_t c = col(i0 + u * Geo::kVTok + lane / Geo::kVlanes);
+      x.v[u] = load16(rv, c < cap ? c * Geo::kRowB + (lane % Geo::kVlanes) * 16 : kNone);
     }
-    const int32_t t = tok(lane);
-    const uint32_t off = t >= 0 ? plane + col(t) * NB : kNone;
-    if constexpr (D == 128) x.vs = __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0);
-    else x.vs = __builtin_amdgcn_raw_buffer_load_b16(rv, off, 0, 0);
+    const uint32_t c = col(i0 + lane);
+    x.vs = load_vs(c < cap ? plane + c * NB : kNone);
   };
 
   // Scores, online softmax and PV of a block whose first nv tokens are valid.
@@ -164,8 +193,10 @@ attn_kv4_kernel(const AttnArgs a) {
     for (int u = 0; u < Geo::kVLoads; ++u)
       *reinterpret_cast<u32x4*>(lds + (u * Geo::kVTok + lane / Geo::kVlanes) * Geo::kLdsRow +
                                 (lane % Geo::kVlanes) * 16) = x.v[u];
+    // no scale behind the last token: its weight is 0, which an infinite one (a NaN block's) would make a NaN
+    const uint32_t vs = lane < nv ? x.vs : 0u;
 #pragma unroll
-    for (int k = 0; k < NB; ++k) ldss[k * 64 + lane] = mx_scale_value((x.vs >> (8 * k)) & 255u);
+    for (int k = 0; k < NB; ++k) ldss[k * 64 + lane] = mx_scale_value((vs >> (8 * k)) & 255u);
     float s[16];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -175,7 +206,7 @@ attn_kv4_kernel(const AttnArgs a) {
       for (int kk = 0; kk < KK; ++kk)
         sj = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(mx_widen(x.k[j][kk], sc)), qb[kk], sj, 0, 0, 0);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[4 * j + r] = sj[r] * a.qscale;
+      for (int r = 0; r < 4; ++r) s[4 * j + r] = sj[r];
     }
     if (nv < 64) {
 #pragma unroll
@@ -185,10 +216,9 @@ attn_kv4_kernel(const AttnArgs a) {
     float mx = s[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-    mx = fmaxf(m, max_over_groups(mx));
+    mx = fmaxf(m, max_over_groups(mx) * qs);
     if (__builtin_amdgcn_ballot_w64(mx > m)) {    // some column's maximum rose
-      const float alpha = fast_exp2(m - mx);       // 0 from -inf; NaN where both are, mended below
-      const float f = m == -INFINITY ? 0.f : alpha;
+      const float f = m == -INFINITY ? 0.f : fast_exp2(m - mx);
       lsum *= f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
@@ -198,7 +228,7 @@ attn_kv4_kernel(const AttnArgs a) {
     float p[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      p[e] = fast_exp2(s[e] - ref);
+      p[e] = fast_exp2(fmaf(s[e], qs, -ref));
       lsum += p[e];
     }
     // P' operands: [set][half of the tokens]
@@ -223,33 +253,45 @@ attn_kv4_kernel(const AttnArgs a) {
 
   const bool gathered = (rw.w & kGathered) != 0;
   if (gathered) {
-    for (int32_t i0 = t_begin; i0 < t_end; i0 += 64) {
+    for (int32_t i0 = t_begin + 64 * w; i0 < t_end; i0 += 64 * NW) {
       Kv4Block<D> x;
-      issue([&](int32_t i) { return i0 + i < t_end ? a.gather[i0 + i] : -1; }, x);
+      issue_listed(i0, t_end, x);
       block(x, t_end - i0);
     }
   } else {
-    const int32_t c_end = min(t_end, n);
-    if (t_begin < c_end) {
+    // The item's tokens before and after the ring's end, each a run of columns, of
+    // which wave w takes every NW-th block of 64; a block's loads are in flight while
+    // the one before it is computed.
+    const int32_t c_end = min(t_end, n), wrap = (int32_t)(cap - start);
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+      const int32_t t0 = (part == 0 ? t_begin : max(t_begin, wrap)) + 64 * w, t1 = part == 0 ? min(c_end, wrap) : c_end;
+      if (t0 >= t1) continue;
+      uint32_t col = part == 0 ? start + (uint32_t)t0 : (uint32_t)(t0 - wrap);
+      int32_t left = t1 - t0;
       Kv4Block<D> xa, xb;
-      auto tok = [&](int32_t tt) { return [tt, c_end](int32_t i) { return tt + i < c_end ? tt + i : -1; }; };
-      issue(tok(t_begin), xa);
-      for (int32_t tt = t_begin; tt < c_end; tt += 128) {
-        issue(tok(tt + 64), xb);
+      issue(true, col, xa);
+#pragma unroll 1
+      while (true) {
+        issue(left > 64 * NW, col + 64 * NW, xb);
         __builtin_amdgcn_sched_barrier(0);   // keep the loads ahead of the computation
-        block(xa, c_end - tt);
-        if (tt + 64 >= c_end) break;
-        issue(tok(tt + 128), xa);
+        block(xa, left);
+        left -= 64 * NW;
+        if (left <= 0) break;
+        col += 128 * NW;
+        issue(left > 64 * NW, col, xa);
         __builtin_amdgcn_sched_barrier(0);
-        block(xb, c_end - tt - 64);
+        block(xb, left);
+        left -= 64 * NW;
+        if (left <= 0) break;
       }
     }
   }
 
   // The current token, from k_new / v_new in bf16: row 0 of a tile of its own.
-  // Its key and value are then quantised into the ring (of a gathered item, by
-  // its first wave): lane i < D / 8 has K's elements 8 i .., the next D / 8 lanes V's.
-  if (gathered ? (rw.w & kCurrent) != 0 && w == 0 : n >= t_begin && n < t_end) {
+  // Its key and value are then quantised into the ring (by
+  // the item's first wave): lane i < D / 8 has K's elements 8 i .., the next D / 8 lanes V's.
+  if (w == 0 && (gathered ? (rw.w & kCurrent) != 0 : n >= t_begin && n < t_end)) {
     const u32x4* knew = reinterpret_cast<const u32x4*>(a.knew) + (bt * a.n_kv_heads + h) * VPT;
     const u32x4* vnew = reinterpret_cast<const u32x4*>(a.vnew) + (bt * a.n_kv_heads + h) * VPT;
     f32x4 sj = {0.f, 0.f, 0.f, 0.f};
@@ -258,7 +300,7 @@ attn_kv4_kernel(const AttnArgs a) {
       const u32x4 kw = c16 == 0 ? knew[KK * g4 + kk] : u32x4{0, 0, 0, 0};
       sj = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kw), qb[kk], sj, 0, 0, 0);
     }
-    const float s = g4 == 0 ? sj[0] * a.qscale : -INFINITY;
+    const float s = g4 == 0 ? sj[0] * qs : -INFINITY;
     const float mx = fmaxf(m, max_over_groups(s));
     const float ref = mx == -INFINITY ? 0.f : mx;
     const float f = m == -INFINITY ? 0.f : fast_exp2(m - ref);

@@ -3,7 +3,7 @@
 #pragma once
 
 #ifndef BATON_KV4_WAVES
-#define BATON_KV4_WAVES 2
+#define BATON_KV4_WAVES 4   // waves per attention workgroup
 #endif
 
 bool is_kv4(const baton_cache* c) { return c->d.dtype == BATON_MXFP4; }
@@ -100,6 +100,28 @@ baton_status append_prompts4_d(const baton_cache* c, const baton::PrefillArgs& p
 
 baton_status append_prompts4(const baton_cache* c, const baton::PrefillArgs& p, hipStream_t s) {
   return c->d.head_dim == 64 ? append_prompts4_d<64>(c, p, s) : append_prompts4_d<128>(c, p, s);
+}
+
+// Automatic split.  A token's bytes are 17/64 of bf16's, so an item costs as
+// much besides them as one of a quarter of the tokens would there: items are
+// longer.  A workgroup of four waves with two blocks each in flight takes what a
+// CU can, so an item per CU is enough (tokens / 256); and a row of n tokens in n / S
+// pieces pays for each piece in the work list and the merge, about 0.25 us a
+// piece, against 2 ns per token of an item, balanced at S = sqrt(128 n).  us per
+// layer at S and at 256 tokens: one row of 32,768 over one kv-head 23.5 (2048) and
+// 42.9, of 100,000 over eight 36 (3584) and 131, of 8192 over 32 18.7 (1024) and
+// 26.9; 32 rows of up to 2048 over 32 38.7 (4096) and 52.6.
+int32_t kv4_split(const baton_cache* c) {
+  const baton::HoleList hl = hole_list(c);
+  int64_t total = 0, longest = 0;
+  for (int32_t b = 0; b < c->d.batch; ++b)
+    if (c->lens[b] > 0 && c->plen[b] == 0) {
+      const int64_t n = row_tokens(c, b, hl) + 1;
+      total += n;
+      longest = std::max(longest, n);
+    }
+  const int64_t s = std::max((total * c->d.n_kv_heads + 255) / 256, (int64_t)std::sqrt(128.0 * (double)longest));
+  return (int32_t)std::min(kAutoSplitMax, std::max(kAutoSplitMin, (s + 63) / 64 * 64));
 }
 
 template <int D, int G>
