@@ -16,17 +16,23 @@
 //
 // One workgroup of 16 waves per row.  The row is read once from memory into LDS (what
 // does not fit is read again); wave w owns the w-th of 16 contiguous parts of
-// it, 16 bytes per lane and step.
-//  * prefixes: 1024 bins of equal width over the top of the values' range hold counts
-//    and weights (floats' own bits would put most tokens into a few bins, whose
-//    atomics then queue); a scan finds the bin in which a prefix ends; that
-//    bin's tokens, a few dozen, are sorted in LDS.  More than fit (equal
-//    logits, mostly) are first narrowed by bins over the bits of their floats, and if
-//    one value alone has too many, its tokens are counted off in order of index.
-//  * the draw: kept weights per wave, then the tokens of the wave's part in
-//    which the target lies.
-// exp: 2^(j / 64) from a table, times a polynomial of degree 5 on half a step: relative
-// error below 2^-53, in about 20 instructions.
+// it, 16 bytes per lane and step.  What bounds it is the vector ALUs of one compute
+// unit -- a weight takes about 25 instructions, a row of 32,000 all weighed 5 us --
+// and the latency of its dependent steps, so whole passes over the row are kept few
+// and a list of tokens in LDS takes their place as soon as one can:
+//  * top_k up to 512: the k-th largest of the threads' own largest values bounds
+//    the k-th largest from below; the tokens from there on, a few more than k, are
+//    the list.
+//  * else 1024 bins of equal width over the top of the values' range hold counts
+//    or weights (floats' own bits would put most tokens into a few bins, whose atomics
+//    then queue); a scan finds the bin in which a prefix ends, and that bin's
+//    tokens, a few dozen, are the list that gives the place exactly.  More than fit
+//    (equal logits, mostly) are first narrowed by bins over the bits of their floats,
+//    and if one value alone has too many, its tokens are counted off in order of index.
+//  * the draw: from a list of the kept tokens where they fit one, else kept
+//    weights per wave, then the tokens of the wave's part in which the target lies.
+// exp: 2^(j / 128) from a table, times a polynomial of degree 4 on half a step:
+// relative error below 2^-49.
 #pragma once
 
 #include "common.hpp"
@@ -36,8 +42,11 @@ namespace {
 
 constexpr int kSampleThreads = 1024, kSampleWaves = kSampleThreads / kWave;
 constexpr int kSampleBins = 1024;        // == kSampleThreads: a bin per thread
-constexpr int kSampleList = 2048;        // tokens sorted at most
-constexpr int kSampleRowBytes = 112 << 10;   // of a row kept in LDS
+constexpr int kSampleList = 2048;        // tokens in a list at most, two per thread
+constexpr int kSampleRank = 192;         // up to here a list is ordered by counting, not sorted
+constexpr int kSampleTopK = 512;         // the largest top_k for which threads' largest values bound it
+constexpr int kSampleQuarters = 4;       // of the row, with bins of their own
+constexpr int kSampleRowBytes = 80 << 10;    // of a row kept in LDS
 
 struct SampleArgs {
   const uint8_t* logits;
@@ -51,24 +60,30 @@ struct SampleArgs {
   int32_t* tokens;
 };
 
-// Floats as unsigned numbers of the same order (no NaN, no -0).
+// Floats (no NaN) as unsigned numbers of the same order, -0 as 0.
 __device__ __forceinline__ uint32_t float_key(float f) {
-  const uint32_t b = __float_as_uint(f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  const uint32_t b = __float_as_uint(f + 0.f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_float(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
 
-__device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t x, int m) {
-  return (uint64_t)__shfl_xor((uint32_t)(x >> 32), m, kWave) << 32 | __shfl_xor((uint32_t)x, m, kWave);
+// One step of a wave's prefix sum: x plus the value DPP moves here (0 from outside).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp_add(uint64_t x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xF, false);
+  return x + ((uint64_t)hi << 32 | lo);
 }
-__device__ __forceinline__ uint64_t shfl_up_u64(uint64_t x, int d) {
-  return (uint64_t)__shfl_up((uint32_t)(x >> 32), d, kWave) << 32 | __shfl_up((uint32_t)x, d, kWave);
-}
-__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t x) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) x += shfl_xor_u64(x, m);
+// Inclusive prefix sum over the wave: within rows of 16 lanes, then across them.
+__device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
+  x = dpp_add<0x111, 0xF>(x);   // row_shr 1, 2, 4, 8
+  x = dpp_add<0x112, 0xF>(x);
+  x = dpp_add<0x114, 0xF>(x);
+  x = dpp_add<0x118, 0xF>(x);
+  x = dpp_add<0x142, 0xA>(x);   // lane 15 of each row into the next (rows 1 and 3)
+  x = dpp_add<0x143, 0xC>(x);   // lane 31 into the upper half
   return x;
 }
 
@@ -93,15 +108,6 @@ struct SampleRow {
   int32_t vocab, n_vec, n_lds;
   u32x4* lds;
 
-  __device__ __forceinline__ void widen(int32_t i, const u32x4& w, float (&x)[EPV]) const {
-    Lane16<T>::widen(w, x);
-#pragma unroll
-    for (int e = 0; e < EPV; ++e) {
-      const int32_t at = i * EPV - off + e;
-      // outside the row: NaN, which every comparison leaves out; -0 as 0
-      x[e] = at >= 0 && at < vocab ? x[e] + 0.f : __uint_as_float(0x7FC00000u);
-    }
-  }
   // A vector from memory; at the row's ends only the elements that are the row's.
   __device__ __forceinline__ u32x4 fetch(int32_t i) const {
     const int32_t at = i * EPV - off;
@@ -115,50 +121,422 @@ struct SampleRow {
       }
     return u32x4{w[0], w[1], w[2], w[3]};
   }
-  __device__ __forceinline__ u32x4 load(int32_t i) const { return i < n_lds ? lds[i] : fetch(i); }
+  // Whether the 64 vectors from i0 on hold elements of the row only.
+  __device__ __forceinline__ bool inside(int32_t i0) const { return i0 > 0 && (i0 + kWave) * EPV - off <= vocab; }
+  // The elements of vector i; outside the row NaN, which every comparison leaves out.
+  __device__ __forceinline__ void widen(int32_t i, const u32x4& w, bool all, float (&x)[EPV]) const {
+    Lane16<T>::widen(w, x);
+    if (all) return;
+#pragma unroll
+    for (int e = 0; e < EPV; ++e) {
+      const int32_t at = i * EPV - off + e;
+      if (at < 0 || at >= vocab) x[e] = __uint_as_float(0x7FC00000u);
+    }
+  }
+  __device__ __forceinline__ uint32_t index(int32_t i, int e) const { return (uint32_t)(i * EPV - off + e); }
 };
 
 struct SampleShared {
-  double table[64];
-  uint64_t weight[kSampleBins];
+  double table[128];             // 2^(i / 128 + shift)
+  uint64_t weight[kSampleQuarters][kSampleBins];
   uint32_t count[kSampleBins];
-  uint64_t list[kSampleList];
-  uint64_t scan[kSampleWaves];
-  uint64_t part[kSampleWaves];
+  uint64_t list[kSampleList];    // tokens: (float_key, ~index), so that larger is earlier
+  uint64_t lw[kSampleList];      // their weights
+  uint64_t scan[2][kSampleWaves];
+  uint64_t part[kSampleWaves], quarter[kSampleQuarters];
   float fmax[kSampleWaves], fmin[kSampleWaves];
   uint32_t kmin, kmax, n_list;
-  int32_t found, found_at;
-  uint64_t before;
-  uint32_t key, index;
+  int32_t found, bin_whole;   // bin_whole: the cut's bin, if its tokens were one list; else -1
+  uint64_t before, weight_before;
+  uint64_t cut;                  // the last kept token
+  uint32_t index;
 };
 
-// Inclusive prefix sum over the workgroup; `total` gets the whole.
-__device__ __forceinline__ uint64_t wg_scan(SampleShared& s, uint64_t x, uint64_t& total) {
-  const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+template <typename T>
+struct Sampler {
+  static constexpr int EPV = Lane16<T>::kElems;
+  SampleShared& s;
+  SampleRow<T> row;
+  int32_t per, v0, v1;        // vectors of a wave's part; this wave's
+  float mx, mn;               // the largest value and the smallest that is finite
+  bool infinite;              // the largest was infinite: see get
+  float per_bin;
+  double scale, top, least, floor_w;   // floor_w: min_p as a weight
+  int tid, lane, w, turn = 0;
+
+  // Inclusive prefix sum over the workgroup; `total` gets the whole.
+  __device__ __forceinline__ uint64_t wg_scan(uint64_t x, uint64_t& total) {
+    x = wave_scan(x);
+    turn ^= 1;                           // alternating, so that one barrier will do
+    if (lane == kWave - 1) s.scan[turn][w] = x;
+    __syncthreads();
+    uint64_t t = lane < kSampleWaves ? s.scan[turn][lane] : 0;
+    t = dpp_add<0x111, 0xF>(t);
+    t = dpp_add<0x112, 0xF>(t);
+    t = dpp_add<0x114, 0xF>(t);
+    t = dpp_add<0x118, 0xF>(t);          // lanes 0 .. 15: sums up to wave `lane`
+    auto from = [&](int l) {
+      return (uint64_t)__builtin_amdgcn_readlane((int)(t >> 32), l) << 32 |
+             (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)t, l);
+    };
+    total = from(kSampleWaves - 1);
+    return x + (w > 0 ? from(w - 1) : 0);
+  }
+
+  // The weight of a value, before it is rounded to a whole number.
+  __device__ __forceinline__ double weight(float x) const {
+    const double y = fmax(((double)x - top) * scale, least);        // 128 log2 w; a NaN is least
+    constexpr double kMagic = 6755399441055744.0;                   // 1.5 * 2^52: rounds to a whole number
+    const double t = y + kMagic;
+    const uint32_t j = (uint32_t)__double_as_longlong(t);
+    const double f = y - (t - kMagic);
+    constexpr double c = 0.0054152123481245727;                     // ln 2 / 128
+    double p = fma(f, c * c * c * c / 24.0, c * c * c / 6.0);
+    p = fma(p, f, c * c / 2.0);
+    p = fma(p, f, c);
+    p = fma(p, f, 1.0);
+    // 2^(j / 128 + shift): the table's entry with j / 128 added to its exponent
+    const double b = __longlong_as_double(__double_as_longlong(s.table[j & 127]) +
+                                          ((uint64_t)((j << 13) & 0xFFF00000u) << 32));
+    return p * b;
+  }
+  __device__ __forceinline__ uint64_t whole(double wd) const {
+    return (uint64_t)__double_as_longlong(wd + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;   // + 2^52
+  }
+  __device__ __forceinline__ uint32_t valid(float x) const { return x >= mn; }
+  __device__ __forceinline__ uint64_t weight_of(float x) const {
+    const uint64_t g = whole(weight(x));
+    return valid(x) ? g : 0;
+  }
+  // 0 also below min_p (the largest value never is)
+  __device__ __forceinline__ uint64_t weight_if(float x, uint32_t keep) const {
+    const double d = weight(x);
+    const uint64_t g = whole(d);
+    return keep & valid(x) & ((uint32_t)(d >= floor_w) | (uint32_t)(x == mx)) ? g : 0;
+  }
+  __device__ __forceinline__ int bin_of(float x) const {
+    return (int)fminf((mx - x) * per_bin, (float)(kSampleBins - 1));
+  }
+
+  // The elements of vector i0 + lane (i0 the same in the wave), NaN outside the row
+  // and from vector `end` on.  Beside an infinity, 1 for one and NaN for all else.
+  __device__ __forceinline__ void get(int32_t i0, int32_t end, float (&x)[EPV]) const {
+    const int32_t i = i0 + lane;
+    const bool all = row.inside(i0) && i0 + kWave <= end;
+    u32x4 v = {0, 0, 0, 0};
+    if (all) v = i0 + kWave <= row.n_lds ? row.lds[i] : i0 < row.n_lds && i < row.n_lds ? row.lds[i] : row.fetch(i);
+    else if (i < end) v = i < row.n_lds ? row.lds[i] : row.fetch(i);
+    row.widen(i, v, all, x);
+    if (!all && i >= end) {
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const uint64_t y = shfl_up_u64(x, d);
-    x += lane >= d ? y : 0;
+      for (int e = 0; e < EPV; ++e) x[e] = __uint_as_float(0x7FC00000u);
+    }
+    if (infinite) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) x[e] = x[e] == INFINITY ? 1.f : __uint_as_float(0x7FC00000u);
+    }
   }
-  __syncthreads();
-  if (lane == kWave - 1) s.scan[w] = x;
-  __syncthreads();
-  uint64_t before = 0;
-  total = 0;
-  for (int v = 0; v < kSampleWaves; ++v) {
-    before += v < w ? s.scan[v] : 0;
-    total += s.scan[v];
+  // f(i, x) for every vector of the row, each wave its part.
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+    for (int32_t i0 = v0; i0 < v1; i0 += kWave) {
+      float x[EPV];
+      get(i0, v1, x);
+      f(i0 + lane, x);
+    }
   }
-  return before + x;
-}
+  // Tokens of lo <= x <= hi for which pick(i, e, x) into the list; n_list counts
+  // also those past its end.
+  template <typename F>
+  __device__ __forceinline__ void collect(float lo, float hi, F&& pick) {
+    if (tid == 0) s.n_list = 0;
+    __syncthreads();
+    each([&](int32_t i, const float (&x)[EPV]) {
+      uint32_t some = 0;
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) some |= x[e] >= lo && x[e] <= hi ? 1u << e : 0u;
+      while (some) {
+        const int e = __builtin_ctz(some);
+        some &= some - 1;
+        float f = x[0];
+#pragma unroll
+        for (int q = 1; q < EPV; ++q) f = e == q ? x[q] : f;
+        if (!pick(i, e, f)) continue;
+        const uint32_t at = atomicAdd(&s.n_list, 1u);
+        if (at < kSampleList) s.list[at] = (uint64_t)float_key(f) << 32 | (uint32_t)~row.index(i, e);
+      }
+    });
+    __syncthreads();
+  }
+  // Values beside which no token of bins b0 .. b1 lies: bin_of's roundings are off by
+  // 2^-13 of a bin, a float's by 2^-24 of it.
+  __device__ __forceinline__ float bin_low(int b1) const {
+    if (b1 >= kSampleBins - 1) return -INFINITY;
+    const double v = top - (b1 + 1.01) / (double)per_bin;
+    return (float)(v - fabs(v) * 0x1p-22);
+  }
+  __device__ __forceinline__ float bin_high(int b0) const {
+    const double v = top - (b0 - 0.01) / (double)per_bin;
+    return (float)(v + fabs(v) * 0x1p-22);
+  }
+
+  // A thread's tokens of the list with what comes before each in its order.
+  struct Place {
+    uint64_t id, w, before_w;
+    uint32_t before;
+    bool in;
+  };
+  // Weights of the n <= kSampleList tokens of the list, and their places.  A short
+  // list is compared with itself, a longer one sorted (bitonic, largest first).
+  __device__ __forceinline__ void order(uint32_t n, Place (&p)[2]) {
+    if (n > kSampleRank) {
+      uint32_t size = 512;
+      while (size < n) size <<= 1;
+      for (uint32_t i = n + tid; i < size; i += kSampleThreads) s.list[i] = 0;
+      __syncthreads();
+      for (uint32_t k = 2; k <= size; k <<= 1)
+        for (uint32_t j = k >> 1; j > 0; j >>= 1) {
+          const uint32_t i = tid;
+          if (i < size / 2) {
+            const uint32_t l = 2 * i - (i & (j - 1)), h = l + j;
+            const uint64_t x = s.list[l], y = s.list[h];
+            if ((x < y) == ((l & k) == 0)) {
+              s.list[l] = y;
+              s.list[h] = x;
+            }
+          }
+          __syncthreads();
+        }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t i = 2 * tid + e;
+        p[e].in = i < n;
+        p[e].id = p[e].in ? s.list[i] : 0;
+        p[e].before = i;
+        const uint64_t g = weight_of(key_float((uint32_t)(p[e].id >> 32)));
+        p[e].w = p[e].in ? g : 0;
+        if (p[e].in) s.lw[i] = g;
+      }
+      uint64_t total;
+      const uint64_t upto = wg_scan(p[0].w + p[1].w, total);
+      p[1].before_w = upto - p[1].w;
+      p[0].before_w = p[1].before_w - p[0].w;
+      return;
+    }
+    p[1].in = false;
+    p[1].w = p[1].before_w = p[1].id = 0;
+    p[1].before = 0;
+    p[0].in = (uint32_t)tid < n;
+    p[0].id = p[0].in ? s.list[tid] : 0;
+    const uint64_t g = weight_of(key_float((uint32_t)(p[0].id >> 32)));
+    p[0].w = p[0].in ? g : 0;
+    if (p[0].in) s.lw[tid] = g;
+    __syncthreads();
+    uint64_t bw = 0;
+    uint32_t b = 0;
+    if ((uint32_t)(w * kWave) < n)
+      for (uint32_t j = 0; j < n; ++j) {
+        const bool ahead = s.list[j] > p[0].id;
+        b += ahead;
+        bw += ahead ? s.lw[j] : 0;
+      }
+    p[0].before = b;
+    p[0].before_w = bw;
+  }
+
+  __device__ __forceinline__ int quarter_of(uint32_t index) const {
+    return (int)(((int32_t)index + row.off) / EPV / (kSampleWaves / kSampleQuarters * per));
+  }
+
+  // The place at which a prefix ends: the first token, in the order, at which the
+  // running count (BY_WEIGHT: weight) reaches `need`, 1 <= need <= all of it, from the
+  // bins' own values and their running sums.  Sets s.cut to it and s.before to the
+  // weight up to it.
+  __device__ __forceinline__ void select(bool by_weight, uint64_t need, uint64_t mine, uint64_t upto,
+                                         uint64_t weight_upto) {
+    __syncthreads();
+    if (upto >= need && upto - mine < need) {    // one thread
+      s.found = tid;
+      s.before = upto - mine;
+      s.weight_before = weight_upto;
+    }
+    if (tid < kSampleQuarters) s.quarter[tid] = 0;
+    __syncthreads();
+    const int bin = s.found;
+    uint64_t before = s.before, weight_before = s.weight_before;
+    collect(bin_low(bin), bin_high(bin), [&](int32_t, int, float x) { return x >= mn && bin_of(x) == bin; });
+    uint32_t n = s.n_list, lo = 0, hi = 0;
+    if (tid == 0) s.bin_whole = n <= kSampleList ? bin : -1;
+    if (n > kSampleList) {
+      // Too many: bins over the keys of [lo, hi] until the list holds them or one key is left.
+      if (tid == 0) {
+        s.kmin = 0xFFFFFFFFu;
+        s.kmax = 0;
+      }
+      __syncthreads();
+      lo = 0xFFFFFFFFu;
+      each([&](int32_t, const float (&x)[EPV]) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+          if (valid(x[e]) && bin_of(x[e]) == bin) {
+            lo = min(lo, float_key(x[e]));
+            hi = max(hi, float_key(x[e]));
+          }
+      });
+      if (lo <= hi) {
+        atomicMin(&s.kmin, lo);
+        atomicMax(&s.kmax, hi);
+      }
+      __syncthreads();
+      lo = s.kmin;
+      hi = s.kmax;
+      while (n > kSampleList && lo < hi) {
+        const int sh = max(0, 22 - __clz((int)(hi - lo)));     // (hi - lo) >> sh < 1024
+        s.weight[0][tid] = 0;
+        s.count[tid] = 0;
+        __syncthreads();
+        each([&](int32_t, const float (&x)[EPV]) {
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) {
+            const uint32_t k = float_key(x[e]);
+            if (valid(x[e]) && k >= lo && k <= hi) {
+              atomicAdd(&s.count[(hi - k) >> sh], 1u);
+              atomicAdd(reinterpret_cast<unsigned long long*>(&s.weight[0][(hi - k) >> sh]),
+                        (unsigned long long)weight_of(x[e]));
+            }
+          }
+        });
+        __syncthreads();
+        const uint64_t c = s.count[tid], g = s.weight[0][tid];
+        uint64_t total;
+        const uint64_t tc = wg_scan(c, total), tg = wg_scan(g, total);
+        const uint64_t m = by_weight ? g : c, t = before + (by_weight ? tg : tc);
+        if (t >= need && t - m < need) {
+          s.found = tid;
+          s.before = t - m;
+          s.weight_before = weight_before + tg - g;
+          s.n_list = (uint32_t)c;
+        }
+        __syncthreads();
+        before = s.before;
+        weight_before = s.weight_before;
+        n = s.n_list;
+        const uint32_t top_key = hi - ((uint32_t)s.found << sh);
+        lo = max(lo, top_key - ((1u << sh) - 1));
+        hi = top_key;
+        __syncthreads();
+      }
+      if (n <= kSampleList)
+        collect(key_float(lo), key_float(hi), [&](int32_t, int, float) { return true; });
+    }
+    if (n <= kSampleList) {
+      Place p[2];
+      order(n, p);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint64_t m0 = before + (by_weight ? p[e].before_w : p[e].before), m = by_weight ? p[e].w : 1;
+        if (p[e].in && m0 < need && m0 + m >= need) {
+          s.cut = p[e].id;
+          s.before = weight_before + p[e].before_w + p[e].w;
+        }
+        // this bin's share of what each quarter keeps
+        if (p[e].w && m0 < need && s.bin_whole >= 0)
+          atomicAdd(reinterpret_cast<unsigned long long*>(&s.quarter[quarter_of(~(uint32_t)p[e].id)]), (unsigned long long)p[e].w);
+      }
+      __syncthreads();
+      return;
+    }
+    // One value alone: its tokens counted off in order of index.
+    const uint64_t value = weight_of(key_float(lo));
+    const uint64_t left = need - before;
+    const uint64_t nth = by_weight ? (left + value - 1) / value : left;      // of them, from 1
+    uint64_t wave_n = 0, total;
+    each([&](int32_t, const float (&x)[EPV]) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) wave_n += valid(x[e]) && float_key(x[e]) == lo;
+    });
+    wave_n = wave_scan(wave_n);
+    if (lane == kWave - 1) s.part[w] = wave_n;
+    __syncthreads();
+    uint64_t seen = 0;
+    int part = 0;
+    while (part < kSampleWaves - 1 && seen + s.part[part] < nth) seen += s.part[part++];
+    const int32_t p1 = min((part + 1) * per, row.n_vec);
+    for (int32_t base = part * per; base < p1; base += kSampleThreads) {
+      const int32_t i0 = base + w * kWave, i = i0 + lane;
+      float x[EPV];
+      uint64_t c = 0;
+      get(i0, p1, x);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) c += valid(x[e]) && float_key(x[e]) == lo;
+      const uint64_t to = seen + wg_scan(c, total);
+      if (to >= nth && to - c < nth) {
+        uint64_t at = to - c;
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+          if (valid(x[e]) && float_key(x[e]) == lo && ++at == nth)
+            s.cut = (uint64_t)lo << 32 | (uint32_t)~row.index(i, e);
+      }
+      seen += total;
+    }
+    if (tid == 0) s.before = weight_before + nth * value;
+    __syncthreads();
+  }
+
+  // The draw from the tokens of the list with weight g[e] (0: not kept) in the places i[e].
+  __device__ __forceinline__ void draw_list(uint32_t n, float u, const uint64_t (&id)[2], const uint64_t (&g)[2],
+                                            const uint32_t (&at)[2], int32_t* token) {
+    // 1024 ranges of the index; then the tokens of the range in which the target lies
+    s.weight[0][tid] = 0;
+    __syncthreads();     // and n_list has been read
+    if (tid == 0) s.n_list = 0;
+    const uint32_t per_range = ((uint32_t)row.vocab + kSampleBins - 1) / kSampleBins;
+    uint32_t range[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      range[e] = ~(uint32_t)id[e] / per_range;
+      if (g[e]) atomicAdd(reinterpret_cast<unsigned long long*>(&s.weight[0][range[e]]), (unsigned long long)g[e]);
+      if (at[e] < n) s.lw[at[e]] = g[e];
+    }
+    __syncthreads();
+    const uint64_t mine = s.weight[0][tid];
+    uint64_t total;
+    const uint64_t upto = wg_scan(mine, total);
+    const uint64_t target = times_fraction<false>(u, total);
+    if (upto > target && upto - mine <= target) {
+      s.found = tid;
+      s.before = upto - mine;
+    }
+    __syncthreads();
+    // those of them that lie in the range, gathered (unless they are more than fit)
+    const uint32_t r = (uint32_t)s.found, first = r * per_range;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (g[e] && range[e] == r) {
+        const uint32_t k = atomicAdd(&s.n_list, 1u);
+        if (k < kSampleBins) s.count[k] = at[e];
+      }
+    __syncthreads();
+    const uint32_t m = s.n_list, few = m <= kSampleBins ? m : n;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (g[e] && range[e] == r) {
+        const uint32_t own = ~(uint32_t)id[e];
+        uint64_t before = s.before;
+        for (uint32_t j = 0; j < few; ++j) {
+          const uint32_t l = m <= kSampleBins ? s.count[j] : j, o = ~(uint32_t)s.list[l];
+          before += o >= first && o < own ? s.lw[l] : 0;
+        }
+        if (before <= target && before + g[e] > target) *token = (int32_t)own;
+      }
+  }
+};
 
 template <typename T>
 __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs a) {
   constexpr int EPV = Lane16<T>::kElems;
   extern __shared__ __attribute__((aligned(16))) u32x4 row_lds[];
   __shared__ SampleShared s;
-  const int tid = threadIdx.x, lane = tid % kWave;
-  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int64_t r = blockIdx.x;
   SampleRow<T> row;
   row.row = a.logits + r * a.ld * T::kBytes;
@@ -167,29 +545,37 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
   row.n_vec = (row.off + a.vocab + EPV - 1) / EPV;
   row.n_lds = min(row.n_vec, kSampleRowBytes / 16);
   row.lds = row_lds;
-  const int32_t per = (row.n_vec + kSampleWaves - 1) / kSampleWaves;   // vectors of a wave's part
-  const int32_t v0 = w * per, v1 = min(v0 + per, row.n_vec);
+  Sampler<T> p{s, row};
+  const int tid = p.tid = threadIdx.x, lane = p.lane = tid % kWave;
+  const int w = p.w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  p.per = (row.n_vec + kSampleWaves - 1) / kSampleWaves;
+  p.v0 = w * p.per;
+  p.v1 = min(p.v0 + p.per, row.n_vec);
 
   const float temperature = a.temperature ? a.temperature[r] : 1.f;
   const int32_t top_k = a.top_k ? a.top_k[r] : 0;
   const float top_p = a.top_p ? a.top_p[r] : 1.f;
   const float min_p = a.min_p ? a.min_p[r] : 0.f;
-  const float u = a.u[r];
+  const float u_in = a.u[r];
+  const float u = u_in > 0.f ? fminf(u_in, 0x1.fffffep-1f) : 0.f;       // a NaN is 0
 
   // The row into LDS; its largest value and the smallest that is finite.
   float mx = -INFINITY, mn = INFINITY;
-  for (int32_t i = v0 + lane; i < v1; i += kWave) {
+  for (int32_t i0 = p.v0; i0 < p.v1; i0 += kWave) {
+    const int32_t i = i0 + lane;
+    if (i >= p.v1) continue;
     const u32x4 v = row.fetch(i);
     if (i < row.n_lds) row.lds[i] = v;
     float x[EPV];
-    row.widen(i, v, x);
+    row.widen(i, v, row.inside(i0), x);
 #pragma unroll
     for (int e = 0; e < EPV; ++e) {
       mx = fmaxf(mx, x[e]);
       mn = x[e] > -INFINITY ? fminf(mn, x[e]) : mn;
     }
   }
-  if (tid < 64) s.table[tid] = exp2((double)tid / 64.0);
+  const float own = mx;       // this thread's largest
+  if (tid < 128) s.table[tid] = ldexp(exp2((double)tid / 128.0), a.shift);
 #pragma unroll
   for (int m = 1; m < kWave; m <<= 1) {
     mx = fmaxf(mx, __shfl_xor(mx, m, kWave));
@@ -200,7 +586,11 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
     s.fmin[w] = mn;
   }
   if (tid == 0) s.index = 0xFFFFFFFFu;
+#pragma unroll
+  for (int q = 0; q < kSampleQuarters; ++q) s.weight[q][tid] = 0;
+  s.count[tid] = 0;
   __syncthreads();
+#pragma unroll
   for (int v = 0; v < kSampleWaves; ++v) {
     mx = fmaxf(mx, s.fmax[v]);
     mn = fminf(mn, s.fmin[v]);
@@ -209,334 +599,217 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
     if (tid == 0) a.tokens[r] = -1;
     return;
   }
+  p.infinite = mx == INFINITY;             // beside an infinity nothing finite has weight
+  if (p.infinite) mx = mn = 1.f;
   if (!(temperature > 0.f) || top_k == 1 || min_p > 1.f) {     // the first of the largest
-    for (int32_t i = v0 + lane; i < v1; i += kWave) {
-      float x[EPV];
-      row.widen(i, row.load(i), x);
+    p.each([&](int32_t i, const float (&x)[EPV]) {
+      uint32_t first = 0xFFFFFFFFu;
 #pragma unroll
-      for (int e = EPV - 1; e >= 0; --e)
-        if (x[e] == mx) atomicMin(&s.index, (uint32_t)(i * EPV - row.off + e));
-    }
+      for (int e = EPV - 1; e >= 0; --e) first = x[e] == mx ? row.index(i, e) : first;
+      if (first != 0xFFFFFFFFu) atomicMin(&s.index, first);
+    });
     __syncthreads();
     if (tid == 0) a.tokens[r] = (int32_t)s.index;
     return;
   }
-  if (mx == INFINITY) mn = INFINITY;   // beside an infinity nothing finite has weight
+  p.mx = mx;
+  p.mn = mn;
+  p.top = (double)mx;
+  p.scale = 128.0 * 1.4426950408889634074 / (double)temperature;
+  p.least = -128.0 * (a.shift + 2);        // a weight that rounds to 0
+  const bool want_m = min_p > 0.f;
+  p.floor_w = want_m ? ldexp((double)min_p, a.shift) : -1.0;
+  // Bins over the top of the range: past 32 T below the maximum a weight is under 2^-46.
+  const float span = fminf(mx - p.mn, 32.f * temperature);
+  p.per_bin = span > 0.f ? fminf((float)(kSampleBins - 1) / span, 3.4e38f) : 0.f;
 
-  // The weight of a value, as a whole number: 0 for what is not >= mn (a NaN, -inf).
-  const double scale = 64.0 * 1.4426950408889634074 / (double)temperature, top = (double)mx;
-  const double unit = __longlong_as_double((int64_t)(1023 + a.shift) << 52);
-  const double least = -64.0 * (a.shift + 2);
-  auto weight_of = [&](float x) -> uint64_t {
-    const double d = x == mx ? 0.0 : (double)x - top;
-    const double y = d * scale;                                     // 64 log2 w
-    if (!(y > least)) return 0;
-    const double magic = 6755399441055744.0;                        // 1.5 * 2^52: rounds to a whole number
-    const double t = y + magic;
-    const int32_t j = (int32_t)__double_as_longlong(t);
-    const double f = (y - (t - magic)) * 0.010830424696249145;      // ln 2 / 64
-    double p = fma(f, 1.0 / 120.0, 1.0 / 24.0);
-    p = fma(p, f, 1.0 / 6.0);
-    p = fma(p, f, 0.5);
-    p = fma(p, f, 1.0);
-    p = fma(p, f, 1.0);
-    const double b = s.table[j & 63];
-    const double pow2 = __longlong_as_double(__double_as_longlong(b) + ((int64_t)(j >> 6) << 52));
-    const double z = fma(p * unit, pow2, 4503599627370496.0);       // + 2^52: rounded to a whole number
-    return (uint64_t)__double_as_longlong(z) & 0xFFFFFFFFFFFFFull;
-  };
-  auto valid = [&](float x) { return x >= mn; };
-
-  // Tokens kept: key above s_key, or equal to it and index at most s_index.
-  uint32_t cut_key = 0, cut_index = 0xFFFFFFFFu;
-  const bool want_k = top_k > 0 && top_k < a.vocab, want_p = top_p < 1.f;
-  if (want_k || want_p) {
-    // Bins over the top of the range: past 32 T below the maximum a weight is under 2^-46.
-    const float span = fminf(mx - mn, 32.f * temperature);
-    const float per_bin = span > 0.f ? (float)(kSampleBins - 1) / span : 0.f;
-    auto bin_of = [&](float x) -> int {
-      return x == mx ? 0 : (int)fminf((mx - x) * per_bin, (float)(kSampleBins - 1));
-    };
-    s.weight[tid] = 0;
+  const bool want_k = top_k > 0 && top_k < a.vocab;
+  const bool want_p = top_p < 1.f;
+  uint64_t cut = 0;       // tokens kept: list ids from here on
+  uint64_t total;
+  if (want_k && top_k <= kSampleTopK) {
+    // A bin that holds or follows the k-th largest of the threads' largest values: at
+    // least k tokens lie up to it.
+    const float first = p.infinite ? (own == INFINITY ? 1.f : -INFINITY) : own;
+    if (p.valid(first)) atomicAdd(&s.count[p.bin_of(first)], 1u);
+    __syncthreads();
+    const uint64_t c = s.count[tid], to = p.wg_scan(c, total);
+    if (tid == 0) s.found = kSampleBins;
+    __syncthreads();
+    if (to >= (uint64_t)top_k && to - c < (uint64_t)top_k) s.found = tid;
+    __syncthreads();
+    const int bin = s.found;       // (fewer threads with a valid value than k: every bin)
     s.count[tid] = 0;
-    __syncthreads();
-    for (int32_t i = v0 + lane; i < v1; i += kWave) {
-      float x[EPV];
-      row.widen(i, row.load(i), x);
+    p.collect(fmaxf(p.bin_low(bin), mn), mx, [&](int32_t, int, float x) { return p.bin_of(x) <= bin; });
+    const uint32_t n = s.n_list;
+    if (n <= kSampleList) {
+      typename Sampler<T>::Place q[2];
+      p.order(n, q);
+      uint64_t g[2], id[2];
+      uint32_t at[2];
+      uint64_t sum = 0;
 #pragma unroll
-      for (int e = 0; e < EPV; ++e)
-        if (valid(x[e])) {
-          const int b = bin_of(x[e]);
-          atomicAdd(&s.count[b], 1u);
-          if (want_p) atomicAdd(reinterpret_cast<unsigned long long*>(&s.weight[b]), (unsigned long long)weight_of(x[e]));
-        }
+      for (int e = 0; e < 2; ++e) {
+        id[e] = q[e].id;
+        at[e] = n > kSampleRank ? 2 * tid + e : e == 0 ? tid : kSampleList;
+        g[e] = q[e].in && q[e].before < (uint32_t)top_k ? q[e].w : 0;
+        sum += g[e];
+      }
+      p.wg_scan(sum, total);
+      const uint64_t need = !want_p ? ~0ull : top_p > 0.f ? times_fraction<true>(top_p, total) : 1;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (q[e].before_w >= max(need, (uint64_t)1)) g[e] = 0;
+        if (want_m && g[e] && !p.weight_if(key_float((uint32_t)(id[e] >> 32)), true)) g[e] = 0;
+      }
+      p.draw_list(n, u, id, g, at, a.tokens + r);
+      return;
     }
+  }
+  if (want_k || want_p) {
+    uint64_t* const weights = s.weight[w / (kSampleWaves / kSampleQuarters)];
+    p.each([&](int32_t, const float (&x)[EPV]) {
+#pragma unroll
+      for (int h = 0; h < EPV; h += 4) {
+        if (want_p) {
+          uint64_t g[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) g[e] = p.weight_of(x[h + e]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (g[e])
+              atomicAdd(reinterpret_cast<unsigned long long*>(&weights[p.bin_of(x[h + e])]), (unsigned long long)g[e]);
+        }
+        if (want_k) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (p.valid(x[h + e])) atomicAdd(&s.count[p.bin_of(x[h + e])], 1u);
+        }
+      }
+    });
     __syncthreads();
-    const uint64_t bin_count = s.count[tid], bin_weight = s.weight[tid];
-    uint64_t all_count, all_weight;
-    const uint64_t to_count = wg_scan(s, bin_count, all_count);
-    const uint64_t to_weight = wg_scan(s, bin_weight, all_weight);
-
-    // The place at which a prefix ends: the first token, in the order, at which the
-    // running count (BY_WEIGHT: weight) reaches `need`, 1 <= need <= all of it.
-    // Sets s.key and s.index to it and s.before to the weight up to it.
-    auto select = [&](bool by_weight, uint64_t need) {
-      const uint64_t mine = by_weight ? bin_weight : bin_count, upto = by_weight ? to_weight : to_count;
-      __syncthreads();
-      if (upto >= need && upto - mine < need) {    // one thread
-        s.found = tid;
-        s.before = upto - mine;
-        s.part[0] = to_weight - bin_weight;
-        s.kmin = 0xFFFFFFFFu;
-        s.kmax = 0;
-        s.n_list = 0;
-      }
-      __syncthreads();
-      const int bin = s.found;
-      uint64_t before = s.before, weight_before = s.part[0];
-      // its tokens into the list, and the range of their keys
-      uint32_t lo = 0xFFFFFFFFu, hi = 0;
-      for (int32_t i = v0 + lane; i < v1; i += kWave) {
-        float x[EPV];
-        row.widen(i, row.load(i), x);
+    const uint64_t bin_count = s.count[tid];
+    uint64_t bin_weight = 0;
 #pragma unroll
-        for (int e = 0; e < EPV; ++e)
-          if (valid(x[e]) && bin_of(x[e]) == bin) {
-            const uint32_t k = float_key(x[e]);
-            lo = min(lo, k);
-            hi = max(hi, k);
-            const uint32_t at = atomicAdd(&s.n_list, 1u);
-            if (at < kSampleList) s.list[at] = (uint64_t)k << 32 | (uint32_t)~(i * EPV - row.off + e);
-          }
+    for (int q = 0; q < kSampleQuarters; ++q) bin_weight += s.weight[q][tid];
+    uint64_t all_count, kept;
+    const uint64_t to_weight = p.wg_scan(bin_weight, kept);
+    const uint64_t to_count = p.wg_scan(bin_count, all_count);
+    // the prefix by count, then the one by weight of what that keeps
+#pragma unroll 1
+    for (int by_weight = 0; by_weight < 2; ++by_weight) {
+      uint64_t need = (uint64_t)top_k;
+      if (by_weight) {
+        if (!want_p) break;
+        need = top_p > 0.f ? max(times_fraction<true>(top_p, kept), (uint64_t)1) : 1;
+      } else if (!want_k || need >= all_count) {
+        continue;
       }
-      if (lo <= hi) {
-        atomicMin(&s.kmin, lo);
-        atomicMax(&s.kmax, hi);
-      }
-      __syncthreads();
-      lo = s.kmin;
-      hi = s.kmax;
-      uint32_t n = s.n_list;
-      // Too many: bins over the keys of [lo, hi] until the list holds them or one key is left.
-      while (n > kSampleList && lo < hi) {
-        const int sh = max(0, 22 - __clz((int)(hi - lo)));     // (hi - lo) >> sh < 1024
-        __syncthreads();
-        s.weight[tid] = 0;
-        s.count[tid] = 0;
-        __syncthreads();
-        for (int32_t i = v0 + lane; i < v1; i += kWave) {
-          float x[EPV];
-          row.widen(i, row.load(i), x);
-#pragma unroll
-          for (int e = 0; e < EPV; ++e)
-            if (valid(x[e])) {
-              const uint32_t k = float_key(x[e]);
-              if (k >= lo && k <= hi) {
-                atomicAdd(&s.count[(hi - k) >> sh], 1u);
-                atomicAdd(reinterpret_cast<unsigned long long*>(&s.weight[(hi - k) >> sh]),
-                          (unsigned long long)(want_p ? weight_of(x[e]) : 0));
-              }
-            }
-        }
-        __syncthreads();
-        const uint64_t c = s.count[tid], g = s.weight[tid];
-        uint64_t total;
-        const uint64_t tc = wg_scan(s, c, total), tg = wg_scan(s, g, total);
-        const uint64_t m = by_weight ? g : c, t = before + (by_weight ? tg : tc);
-        __syncthreads();
-        if (t >= need && t - m < need) {
-          s.found = tid;
-          s.before = t - m;
-          s.part[0] = weight_before + tg - g;
-          s.n_list = (uint32_t)c;
-        }
-        __syncthreads();
-        before = s.before;
-        weight_before = s.part[0];
-        n = s.n_list;
-        const uint32_t top_key = hi - ((uint32_t)s.found << sh);
-        lo = max(lo, top_key - ((1u << sh) - 1));
-        hi = top_key;
-        __syncthreads();
-        if (n <= kSampleList) {      // the list, now that they fit
-          if (tid == 0) s.n_list = 0;
-          __syncthreads();
-          for (int32_t i = v0 + lane; i < v1; i += kWave) {
-            float x[EPV];
-            row.widen(i, row.load(i), x);
-#pragma unroll
-            for (int e = 0; e < EPV; ++e)
-              if (valid(x[e])) {
-                const uint32_t k = float_key(x[e]);
-                if (k >= lo && k <= hi) {
-                  const uint32_t at = atomicAdd(&s.n_list, 1u);
-                  if (at < kSampleList) s.list[at] = (uint64_t)k << 32 | (uint32_t)~(i * EPV - row.off + e);
-                }
-              }
-          }
-          __syncthreads();
-        }
-      }
-      if (n <= kSampleList) {
-        // Sort the list, largest first (bitonic; filled up with zeros).
-        uint32_t size = 2;
-        while (size < n) size <<= 1;
-        for (uint32_t i = tid; i < size; i += kSampleThreads)
-          if (i >= n) s.list[i] = 0;
-        __syncthreads();
-        for (uint32_t k = 2; k <= size; k <<= 1)
-          for (uint32_t j = k >> 1; j > 0; j >>= 1) {
-            for (uint32_t i = tid; i < size / 2; i += kSampleThreads) {
-              const uint32_t p = 2 * i - (i & (j - 1)), q = p + j;
-              const uint64_t x = s.list[p], y = s.list[q];
-              if ((x < y) == ((p & k) == 0)) {
-                s.list[p] = y;
-                s.list[q] = x;
-              }
-            }
-            __syncthreads();
-          }
-        // Two neighbours per thread: the first at which the sum reaches `need`.
-        const uint32_t i0 = 2 * tid;
-        uint64_t g[2], m[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const bool in = i0 + e < n;
-          g[e] = in && want_p ? weight_of(key_float((uint32_t)(s.list[i0 + e] >> 32))) : 0;
-          m[e] = by_weight ? g[e] : in ? 1 : 0;
-        }
-        uint64_t total;
-        const uint64_t tm = before + wg_scan(s, m[0] + m[1], total) - m[1] - m[0];
-        const uint64_t tg = weight_before + wg_scan(s, g[0] + g[1], total) - g[1] - g[0];
-        uint64_t m_at = tm, g_at = tg;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (m_at < need && m_at + m[e] >= need) {
-            s.key = (uint32_t)(s.list[i0 + e] >> 32);
-            s.index = ~(uint32_t)s.list[i0 + e];
-            s.before = g_at + g[e];
-          }
-          m_at += m[e];
-          g_at += g[e];
-        }
-        __syncthreads();
-        return;
-      }
-      // One value alone: its tokens counted off in order of index.
-      const uint64_t each = want_p ? weight_of(key_float(lo)) : 0;
-      const uint64_t left = need - before;
-      const uint64_t nth = by_weight ? (left + each - 1) / each : left;      // of them, from 1
-      uint32_t mine_n = 0;
-      for (int32_t i = v0 + lane; i < v1; i += kWave) {
-        float x[EPV];
-        row.widen(i, row.load(i), x);
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) mine_n += valid(x[e]) && float_key(x[e]) == lo;
-      }
-      const uint64_t wave_n = wave_sum_u64(mine_n);
-      __syncthreads();
-      if (lane == 0) s.part[w] = wave_n;
-      __syncthreads();
-      uint64_t seen = 0;
-      int part = 0;
-      while (part < kSampleWaves - 1 && seen + s.part[part] < nth) seen += s.part[part++];
-      const int32_t p1 = min((part + 1) * per, row.n_vec);
-      for (int32_t base = part * per; base < p1; base += kSampleThreads) {
-        const int32_t i = base + tid;
-        float x[EPV];
-        uint32_t c = 0;
-        if (i < p1) {
-          row.widen(i, row.load(i), x);
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) c += valid(x[e]) && float_key(x[e]) == lo;
-        }
-        uint64_t total;
-        const uint64_t upto = seen + wg_scan(s, c, total);
-        if (upto >= nth && upto - c < nth) {
-          uint64_t at = upto - c;
-#pragma unroll
-          for (int e = 0; e < EPV; ++e)
-            if (valid(x[e]) && float_key(x[e]) == lo && ++at == nth) s.index = (uint32_t)(i * EPV - row.off + e);
-        }
-        seen += total;
-      }
-      if (tid == 0) {
-        s.key = lo;
-        s.before = weight_before + nth * each;
-      }
-      __syncthreads();
-    };
-
-    uint64_t kept = all_weight;
-    if (want_k && (uint64_t)top_k < all_count) {
-      select(false, (uint64_t)top_k);
-      cut_key = s.key;
-      cut_index = s.index;
+      p.select(by_weight != 0, need, by_weight ? bin_weight : bin_count, by_weight ? to_weight : to_count,
+               to_weight - bin_weight);
+      cut = s.cut;
       kept = s.before;
     }
-    if (want_p) {
-      const uint64_t need = top_p > 0.f ? times_fraction<true>(top_p, kept) : 1;
-      select(true, need < 1 ? 1 : need);
-      cut_key = s.key;
-      cut_index = s.index;
-    }
   }
 
-  // Weight of a token if it is kept, else 0.
-  const double floor_p = (double)min_p;
-  auto kept_weight = [&](float x, int32_t at) -> uint64_t {
-    if (!valid(x)) return 0;
-    const uint32_t k = float_key(x);
-    if (k < cut_key || (k == cut_key && (uint32_t)at > cut_index)) return 0;
-    if (min_p > 0.f && x != mx && exp(((double)x - top) / (double)temperature) < floor_p) return 0;
-    return weight_of(x);
+  const uint32_t cut_key = (uint32_t)(cut >> 32), cut_index = ~(uint32_t)cut;
+  const float cut_x = cut ? key_float(cut_key) : mn;
+  auto kept = [&](int32_t i, int e, float x) {
+    return (uint32_t)(x > cut_x) | ((uint32_t)(x == cut_x) & (uint32_t)(row.index(i, e) <= cut_index));
   };
-  uint64_t sum = 0;
-  for (int32_t i = v0 + lane; i < v1; i += kWave) {
-    float x[EPV];
-    row.widen(i, row.load(i), x);
+  // Kept weights of a vector's tokens.
+  auto weigh = [&](int32_t i, const float (&x)[EPV], uint64_t (&g)[EPV]) {
+    if (cut || want_m) {
 #pragma unroll
-    for (int e = 0; e < EPV; ++e) sum += kept_weight(x[e], i * EPV - row.off + e);
-  }
-  sum = wave_sum_u64(sum);
-  __syncthreads();
-  if (lane == 0) s.part[w] = sum;
-  if (tid == 0) s.found_at = -1;
-  __syncthreads();
-  uint64_t total = 0;
-  for (int v = 0; v < kSampleWaves; ++v) total += s.part[v];
-  // the first token at which the running weight exceeds u * total
-  const float uc = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;       // a NaN is 0
-  const uint64_t target = times_fraction<false>(uc, total);
-  uint64_t seen = 0;
-  int part = 0;
-  while (part < kSampleWaves - 1 && seen + s.part[part] <= target) seen += s.part[part++];
-  const int32_t p1 = min((part + 1) * per, row.n_vec);
-  for (int32_t base = part * per; base < p1; base += kSampleThreads) {
-    const int32_t i = base + tid;
-    float x[EPV];
-    uint64_t g[EPV], mine = 0;
+      for (int e = 0; e < EPV; ++e) g[e] = p.weight_if(x[e], kept(i, e, x[e]));
+    } else {
 #pragma unroll
-    for (int e = 0; e < EPV; ++e) g[e] = 0;
-    if (i < p1) {
-      row.widen(i, row.load(i), x);
+      for (int e = 0; e < EPV; ++e) g[e] = p.weight_of(x[e]);
+    }
+  };
+  // The kept weight of parts of the row, in order: its quarters from the bins, where
+  // those and the cut's own bin say it all; else from a list of the kept tokens if
+  // they fit one; else a wave's part each, weighed once more.
+  int32_t p0, p1, parts = kSampleWaves;
+  if (want_p && !want_m && s.bin_whole >= 0) {
+    parts = kSampleQuarters;
+    uint64_t sum = 0;
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        g[e] = kept_weight(x[e], i * EPV - row.off + e);
-        mine += g[e];
+    for (int e = 0; e < 4; ++e) {
+      const int b = w % 4 * 256 + lane * 4 + e;
+      sum += b < s.bin_whole ? s.weight[w / 4][b] : 0;
+    }
+    sum = wave_scan(sum);
+    if (lane == kWave - 1) s.part[w] = sum;
+    __syncthreads();
+    if (tid < kSampleQuarters) {
+      sum = s.quarter[tid];
+      for (int v = 0; v < 4; ++v) sum += s.part[4 * tid + v];
+    }
+    __syncthreads();
+    if (tid < kSampleQuarters) s.part[tid] = sum;
+  } else {
+    if (cut || want_m) {
+      // a value below which min_p keeps nothing: T ln(min_p) under the maximum, and some more
+      const float depth = -1.01f * temperature * logf(fmaxf(min_p, 1e-37f)) + 1e-5f * fabsf(mx) + 1e-30f;
+      const float low = want_m && mx - depth > cut_x ? mx - depth : cut_x;
+      p.collect(low, mx, [&](int32_t i, int e, float x) { return kept(i, e, x) != 0; });
+      const uint32_t n = s.n_list;
+      if (n <= kSampleList) {
+        uint64_t id[2], g[2];
+        uint32_t at[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          at[e] = tid + e * kSampleThreads;
+          const bool in = at[e] < n;
+          id[e] = in ? s.list[at[e]] : 0;
+          const uint64_t v = p.weight_if(key_float((uint32_t)(id[e] >> 32)), in);
+          g[e] = in ? v : 0;
+        }
+        p.draw_list(n, u, id, g, at, a.tokens + r);
+        return;
       }
     }
-    uint64_t all;
-    const uint64_t upto = seen + wg_scan(s, mine, all);
+    uint64_t sum = 0;
+    p.each([&](int32_t i, const float (&x)[EPV]) {
+      uint64_t g[EPV];
+      weigh(i, x, g);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) sum += g[e];
+    });
+    sum = wave_scan(sum);
+    if (lane == kWave - 1) s.part[w] = sum;
+  }
+  __syncthreads();
+  total = 0;
+  for (int v = 0; v < parts; ++v) total += s.part[v];
+  // the first token at which the running weight exceeds u * total
+  const uint64_t target = times_fraction<false>(u, total);
+  uint64_t seen = 0;
+  int part = 0;
+  while (part < parts - 1 && seen + s.part[part] <= target) seen += s.part[part++];
+  const int32_t wide = kSampleWaves / parts * p.per;
+  p0 = part * wide;
+  p1 = min(p0 + wide, row.n_vec);
+  for (int32_t base = p0; base < p1; base += kSampleThreads) {
+    const int32_t i0 = base + w * kWave, i = i0 + lane;
+    float x[EPV];
+    uint64_t g[EPV], mine = 0, all;
+    p.get(i0, p1, x);
+    weigh(i, x, g);
+#pragma unroll
+    for (int e = 0; e < EPV; ++e) mine += g[e];
+    const uint64_t upto = seen + p.wg_scan(mine, all);
     if (upto > target && upto - mine <= target) {
       uint64_t at = upto - mine;
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
-        if (at <= target && at + g[e] > target) a.tokens[r] = i * EPV - row.off + e;
+        if (at <= target && at + g[e] > target) a.tokens[r] = (int32_t)row.index(i, e);
         at += g[e];
       }
     }
     seen += all;
+    if (seen > target) break;
   }
 }
 
