@@ -10,7 +10,8 @@
 //    range's sums go to the workspace in fp32.
 //  * up: the ranges' sums are added in order, scaled, and split into two bf16
 //    halves (the value and what its rounding leaves: 16 bits of it), staged in LDS;
-//    then 16 x 16 tiles of y = h . B^T, every wave its own columns.  The second half
+//    then 16 x 16 tiles of y = h . B^T, every wave its own columns, the next 32
+//    columns of B and of y's first rows on their way meanwhile.  The second half
 //    costs one more matrix operation on operands that are in registers; without it
 //    h would be rounded to 8 bits.
 // Sums are fp32 in a fixed order: the same call gives the same bits.
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_down_kernel(con
       for (int i = 0; i < U; ++i) {
         const int k = 32 * (s + i);
         const bool in = s + i < s1 && k + 8 * g4 < a.K;   // K is a multiple of 8
-        aw[i] = in ? *reinterpret_cast<const u32x4*>(ar + k) : zero;
+        aw[i] = in ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(ar + k)) : zero;
 #pragma unroll
         for (int t = 0; t < NT; ++t) xw[i][t] = in ? *reinterpret_cast<const u32x4*>(xr[t] + k) : zero;
       }
@@ -130,9 +131,17 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_down_kernel(con
     *reinterpret_cast<ad_f32x4*>(a.h + ((int64_t)split * a.rows + first + r) * a.hs + j) = sum;
 }
 
-__global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const AdapterArgs a) {
-  constexpr int ROW = kAdapterMaxRank + 8;     // bf16 elements per staged row, padded
-  __shared__ __attribute__((aligned(16))) uint16_t hs_hi[kAdapterRows * ROW], hs_lo[kAdapterRows * ROW];
+// Elements between two staged rows of h, of NKK 32-wide steps: padded by 16 bytes.
+template <int NKK>
+constexpr int adapter_row() { return 32 * NKK + 8; }
+
+// Ranks up to 32 * NKK; `lds_rows` rows of h (whole tiles of 16) are staged twice
+// in the launch's dynamic LDS.
+template <int NKK>
+__global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const AdapterArgs a, const int32_t lds_rows) {
+  constexpr int ROW = adapter_row<NKK>();
+  extern __shared__ __attribute__((aligned(16))) uint16_t hs_hi[];
+  uint16_t* const hs_lo = hs_hi + lds_rows * ROW;
   const int gi = adapter_group<true>(a, blockIdx.x);
   const AdapterGroup& g = a.g[gi];
   const int local = (int)blockIdx.x - (gi > 0 ? a.g[gi - 1].up_end : 0);
@@ -154,16 +163,41 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
   }
   const int first = g.begin + rb * kAdapterRows;
   const int n = min((gi + 1 < a.n_groups ? a.g[gi + 1].begin : a.end) - first, kAdapterRows);
-  const int rank = g.rank, n_kk = (rank + 31) / 32, n_rt = (n + 15) / 16;
+  const int rank = g.rank, n_rt = (n + 15) / 16;
   const int tid = threadIdx.x, lane = tid % kWave, g4 = lane / 16, c16 = lane % 16;
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const u32x4 zero = {0, 0, 0, 0};
+  const int w0 = c0 + w * a.cols, w1 = min(w0 + a.cols, c_end);
+  // B of 32 columns: row 4 g + r of tile j is column 8 g + 4 j + r, so a lane ends
+  // with 8 neighbouring columns of its batch row.  Columns past the last read it again.
+  auto load_b = [&](int c, u32x4 (&bw)[2][NKK]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int col = min(c + 8 * (c16 / 4) + 4 * j + c16 % 4, c_end - 1);
+      const uint16_t* br = g.b + (int64_t)col * rank + 8 * g4;
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk)
+        bw[j][kk] = 32 * kk + 8 * g4 < rank ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(br + 32 * kk)) : zero;
+    }
+  };
+  // y of the first tile of batch rows at those columns
+  const int64_t y_row = (int64_t)a.row[first + min(c16, n - 1)] * a.N + 8 * g4;
+  auto load_y = [&](int c) {
+    return a.accumulate && c16 < n && c + 8 * g4 < w1 ? *reinterpret_cast<const u32x4*>(a.y + y_row + c) : zero;
+  };
+  u32x4 bw[2][NKK], old = zero;
+  if (w0 < w1) {
+    load_b(w0, bw);
+    old = load_y(w0);
+  }
   // h of the part, four elements per thread and step; zeros up to whole operands
-  const int quads = n_kk * 8;
-  for (int i = tid; i < n_rt * 16 * quads; i += kWave * kAdapterWaves) {
-    const int r = i / quads, j = 4 * (i % quads);
+  constexpr int kQuads = NKK * 8;
+  for (int i = tid; i < n_rt * 16 * kQuads; i += kWave * kAdapterWaves) {
+    const int r = i / kQuads, j = 4 * (i % kQuads);
     ad_f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (r < n && j < rank) {
       const float* src = a.h + (int64_t)(first + r) * a.hs + p * rank + j;
+#pragma unroll 4
       for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const ad_f32x4*>(src + (int64_t)s * a.rows * a.hs);
     }
     uint32_t hi[4], lo[4];
@@ -178,39 +212,28 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
     *reinterpret_cast<uint2*>(hs_lo + r * ROW + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
   }
   __syncthreads();
-  const u32x4 zero = {0, 0, 0, 0};
-  const int w0 = c0 + w * a.cols, w1 = min(w0 + a.cols, c_end);
-  // 32 columns at a time: row 4 g + r of tile j is column 8 g + 4 j + r, so a lane
-  // ends with 8 neighbouring columns of its batch row
   for (int c = w0; c < w1; c += 32) {
-    ad_bf16x8 bv[2][kAdapterMaxRank / 32];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int col = c + 8 * (c16 / 4) + 4 * j + c16 % 4;
-      const uint16_t* br = g.b + (int64_t)min(col, c_end - 1) * rank + 8 * g4;
-#pragma unroll
-      for (int kk = 0; kk < kAdapterMaxRank / 32; ++kk)
-        if (kk < n_kk)
-          bv[j][kk] = ad_vec(32 * kk + 8 * g4 < rank ? *reinterpret_cast<const u32x4*>(br + 32 * kk) : zero);
+    u32x4 next[2][NKK], next_old = zero;
+    if (c + 32 < w1) {      // on their way while these columns are computed
+      load_b(c + 32, next);
+      next_old = load_y(c + 32);
     }
     for (int t = 0; t < n_rt; ++t) {
       const int r = 16 * t + c16;
       const bool ok = r < n && c + 8 * g4 < w1;     // w1 is a multiple of 8
       u32x4* yp = reinterpret_cast<u32x4*>(a.y + (int64_t)a.row[first + min(r, n - 1)] * a.N + c + 8 * g4);
-      u32x4 old = zero;
-      if (ok && a.accumulate) old = *yp;
+      if (t > 0) old = ok && a.accumulate ? *yp : zero;
       ad_f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-      for (int kk = 0; kk < kAdapterMaxRank / 32; ++kk)
-        if (kk < n_kk) {
-          const ad_bf16x8 hi = ad_vec(*reinterpret_cast<const u32x4*>(hs_hi + r * ROW + 32 * kk + 8 * g4));
-          const ad_bf16x8 lo = ad_vec(*reinterpret_cast<const u32x4*>(hs_lo + r * ROW + 32 * kk + 8 * g4));
+      for (int kk = 0; kk < NKK; ++kk) {
+        const ad_bf16x8 hi = ad_vec(*reinterpret_cast<const u32x4*>(hs_hi + r * ROW + 32 * kk + 8 * g4));
+        const ad_bf16x8 lo = ad_vec(*reinterpret_cast<const u32x4*>(hs_lo + r * ROW + 32 * kk + 8 * g4));
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[j][kk], lo, acc[j], 0, 0, 0);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bv[j][kk], hi, acc[j], 0, 0, 0);
-          }
+        for (int j = 0; j < 2; ++j) {
+          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j][kk]), lo, acc[j], 0, 0, 0);
+          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j][kk]), hi, acc[j], 0, 0, 0);
         }
+      }
       u32x4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -218,6 +241,11 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
                f32_to_bf16_rne(bf16_hi(old[e]) + acc[e / 2][2 * (e % 2) + 1]) << 16;
       if (ok) *yp = o;
     }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) bw[j][kk] = next[j][kk];
+    old = next_old;
   }
 }
 

@@ -82,6 +82,7 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
   for (int32_t at = 0; at < n_order;) {
     // the next groups, up to a launch's number of them
     int64_t units = 0;           // workgroups of the down launch for each split
+    int32_t max_rank = 0, lds_rows = 0;
     a.n_groups = 0;
     while (at < n_order && a.n_groups < kAdapterGroups) {
       const int64_t i = (int64_t)(key[at] >> 32) - 1;
@@ -95,13 +96,18 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
       for (; at < n_order && (int64_t)(key[at] >> 32) - 1 == i; ++at) a.row[at] = (uint16_t)key[at];
       const int32_t rbs = (at - from + kAdapterRows - 1) / kAdapterRows;
       g.up_end = rbs;            // row blocks; made into workgroups below
+      max_rank = std::max(max_rank, (int32_t)g.rank);
+      lds_rows = std::max(lds_rows, std::min((at - from + 15) / 16 * 16, (int32_t)kAdapterRows));
       units += (int64_t)rbs * ((n_parts * g.rank + 15) / 16);
     }
     a.end = (int16_t)at;
-    // Ranges of k: about 2048 waves in all, at least four steps of 32 for each wave.
+    // Ranges of k: about 1024 workgroups in all, at least eight steps of 32 (the
+    // loads a wave has in flight at once) for each wave.  us of both launches, 256
+    // rows of 40 adapters of rank 64, 4096 to 2 x 11008: 50.2, with 512 workgroups 53.7;
+    // 64 rows of 24 of rank 32, 4096 to 12288: 15.3, with four steps a wave 16.3.
     const int64_t fit = per_split ? (int64_t)(ws_bytes / per_split) : 1;
-    int64_t splits = units > 0 ? 512 / units : 1;
-    splits = std::max<int64_t>(1, std::min({splits, (int64_t)(steps + 15) / 16, fit, (int64_t)64}));
+    int64_t splits = units > 0 ? 1024 / units : 1;
+    splits = std::max<int64_t>(1, std::min({splits, (int64_t)(steps + 31) / 32, fit, (int64_t)64}));
     a.kt = (int32_t)((steps + splits - 1) / splits);
     a.splits = (steps + a.kt - 1) / a.kt;
     // Columns of y per wave: about 4096 waves in all, 32 to 256 columns.
@@ -123,7 +129,12 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
     }
     const dim3 block(kWave * kAdapterWaves);
     if (down > 0) hipLaunchKernelGGL(adapter_down_kernel, dim3((unsigned)down), block, 0, stream, a);
-    hipLaunchKernelGGL(adapter_up_kernel, dim3((unsigned)up), block, 0, stream, a);
+    auto launch_up = [&](auto kernel, int32_t row) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)up), block, (size_t)lds_rows * row * 2 * sizeof(uint16_t), stream, a, lds_rows);
+    };
+    if (max_rank <= 32) launch_up(adapter_up_kernel<1>, adapter_row<1>());
+    else if (max_rank <= 64) launch_up(adapter_up_kernel<2>, adapter_row<2>());
+    else launch_up(adapter_up_kernel<4>, adapter_row<4>());
     if (hipGetLastError() != hipSuccess) return BATON_EHIP;
   }
   return BATON_OK;
