@@ -6,6 +6,8 @@ baton.py); PyTorch provides the buffers.  The layer is the paper's model's
 each query's token count -> re-batched attention (BatonCache.decode_attn) ->
 output projection added to the residual stream -> RMS norm -> gate/up
 projection -> silu(gate) * up -> down projection added to the residual stream.
+What each query of the batch brings of its own joins it: low-rank adapters
+beside the projections, and its sampling parameters for the next token.
 """
 from . import baton as B
 from .cache import _cur_stream as _stream
@@ -189,11 +191,16 @@ class DecodeLayers:
     once.  Each residual add is fused with the normalisation that follows it (the
     output projection with norm2, the down projection with the next layer's
     norm1), so layer(l + 1) expects x as layer(l) returned it, and the gate/up
-    projection with the gated activation."""
+    projection with the gated activation.
+
+    adapters[layer]: dict from names of PROJ to Adapters (qkv in parts [Hq D, Hkv D,
+    Hkv D], gate_up in [F, F], the same adapter at the same index everywhere);
+    slot_adapter[slot] is the index its query uses, -1 for none, and may be changed
+    between steps.  head: dict of norm [hid] and out [vocab][hid], for next_tokens."""
 
     PROJ = ("qkv", "o", "gate_up", "down")
 
-    def __init__(self, cache, weights, gemm, theta=10000.0, eps=1e-5):
+    def __init__(self, cache, weights, gemm, theta=10000.0, eps=1e-5, adapters=None, head=None):
         import torch
         self.cache, self.w, self.gemm, self.theta, self.eps = cache, weights, gemm, theta, eps
         Bt, Hq, Hkv, D = cache.batch, cache.n_q_heads, cache.n_kv_heads, cache.head_dim
@@ -207,6 +214,23 @@ class DecodeLayers:
         self.q, self.k, self.v, self.att = e(Bt, Hq, D), e(Bt, Hkv, D), e(Bt, Hkv, D), e(Bt, Hq, D)
         self.gu, self.act = e(Bt, 2 * F), e(Bt, F)
         self._normed = None   # (layer, x) whose norm1 input h already holds
+        if adapters is not None and (len(adapters) != len(weights) or any(set(a) - set(self.PROJ) for a in adapters)):
+            raise ValueError(f"adapters: one dict over {self.PROJ} per layer")
+        self.adapters, self.slot_adapter = adapters, [-1] * Bt
+        self.head = None
+        if head is not None:
+            vocab = head["out"].shape[0]
+            self.head, self.head_norm = gemm.pack(head["out"]), head["norm"]
+            self.logits, self.sampler = e(Bt, vocab), Sampler(Bt, vocab)
+
+    def _adapt(self, layer, proj, x, y):
+        """y += the low-rank products of the slots with an adapter of this projection."""
+        ad = self._adapter(layer, proj)
+        if ad is not None:
+            self.gemm.linear_adapters(x, ad, self.slot_adapter, y, accumulate=True)
+
+    def _adapter(self, layer, proj):
+        return None if self.adapters is None or max(self.slot_adapter) < 0 else self.adapters[layer].get(proj)
 
     def layer(self, layer, x):
         """One layer of the decode step on the residual stream x [batch][hid] (in place)."""
@@ -215,15 +239,19 @@ class DecodeLayers:
             rmsnorm(x, w["norm1"], self.h, self.eps)
         self._normed = None
         g.linear_packed(self.h, wp["qkv"], self.qkv)
+        self._adapt(layer, "qkv", self.h, self.qkv)
         rope_qkv(self.cache, self.qkv, self.q, self.k, self.v, self.theta)
         self.cache.decode_attn(layer, self.q, self.k, self.v, out=self.att)
         att = self.att.view(self.att.shape[0], -1)
+        self._adapt(layer, "o", att, x)   # before the projection, whose sum the norm then takes
         g.linear_packed_rmsnorm(att, wp["o"], x, w["norm2"], self.eps, self.h, accumulate=True)
-        if wp["gate_up"].out_dim % 32 == 0:
+        if wp["gate_up"].out_dim % 32 == 0 and self._adapter(layer, "gate_up") is None:
             g.linear_packed_silu(self.h, wp["gate_up"], self.act)
         else:
             g.linear_packed(self.h, wp["gate_up"], self.gu)
+            self._adapt(layer, "gate_up", self.h, self.gu)
             silu_mul(self.gu, self.act)
+        self._adapt(layer, "down", self.act, x)
         if layer + 1 < len(self.w):
             g.linear_packed_rmsnorm(self.act, wp["down"], x, self.w[layer + 1]["norm1"], self.eps, self.h,
                                     accumulate=True)
@@ -231,3 +259,14 @@ class DecodeLayers:
         else:
             g.linear_packed(self.act, wp["down"], x, accumulate=True)
         return x
+
+    def next_tokens(self, x, u, temperature=None, top_k=None, top_p=None, min_p=None):
+        """The next token of every slot (int32 [batch], the Sampler's own tensor; a free
+        slot's says nothing) from the last layer's residual stream x [batch][hid]: norm,
+        vocabulary projection, sampling with each slot's parameters and random number u."""
+        if self.head is None:
+            raise ValueError("next_tokens: no head was given")
+        rmsnorm(x, self.head_norm, self.h, self.eps)
+        self._normed = None
+        self.gemm.linear_packed(self.h, self.head, self.logits)
+        return self.sampler(self.logits, u, temperature, top_k, top_p, min_p)
