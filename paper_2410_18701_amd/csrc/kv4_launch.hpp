@@ -41,7 +41,7 @@ baton_status launch_segs4_d(const baton_cache* c, const std::vector<Seg>& segs, 
       a.kext[used] = static_cast<baton::u32x4*>(const_cast<void*>(g.ks));
       a.vext[used] = static_cast<baton::u32x4*>(const_cast<void*>(g.vs));
       tiles += (int64_t)a.tiles_per_row[used] * 2 * c->d.n_layers * c->d.n_kv_heads;
-      a.tile_end[used] = tiles;
+      a.tile_end[used] = (uint32_t)tiles;
       ++used;
     }
     a.n_segs = used;
@@ -88,7 +88,7 @@ baton_status append_prompts4_d(const baton_cache* c, const baton::PrefillArgs& p
       a.kext[i] = reinterpret_cast<baton::u32x4*>(const_cast<uint32_t*>(p.knew));
       a.vext[i] = reinterpret_cast<baton::u32x4*>(const_cast<uint32_t*>(p.vnew));
       tiles += (int64_t)a.tiles_per_row[i] * 2 * p.n_kv_heads;
-      a.tile_end[i] = tiles;
+      a.tile_end[i] = (uint32_t)tiles;
     }
     if (tiles > 0x7FFFFFFF) return BATON_EINVAL;
     hipLaunchKernelGGL(baton::seg4_kernel<D>, dim3((unsigned)tiles), dim3(baton::kCopyThreads), 0, s, a);

@@ -78,6 +78,14 @@ __device__ __forceinline__ u32x4 mx_widen(uint32_t c, float s) {
   return w;
 }
 
+// The scale bytes of a token from the D / 8 lanes that hold it, in the first of them.
+template <int D>
+__device__ __forceinline__ uint32_t mx_scales(uint32_t s) {
+  s |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x104, 0xF, 0xF, true) << 8;             // row_shl 4
+  if constexpr (D == 128) s |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x108, 0xF, 0xF, true) << 16;
+  return s;
+}
+
 // SegArgs for a 4-bit ring: segments as there, the contiguous side in bf16 with
 // its own strides (a prompt's keys lie [position][head][D], a prefilled query's
 // [layer][head][position][D]).  k, v and layer_vec as in SegArgs.
@@ -94,7 +102,7 @@ struct Seg4Args {
   int32_t len[kMaxSegs];
   int32_t tiles_per_row[kMaxSegs];
   int64_t col0[kMaxSegs];
-  int64_t tile_end[kMaxSegs];
+  uint32_t tile_end[kMaxSegs];
   int32_t dst_slot[kMaxSegs];
   int64_t tok_stride[kMaxSegs];    // 16-byte vectors of the contiguous side: token to token,
   int64_t head_stride[kMaxSegs];   //   head to head (layers n_kv_heads heads apart),
@@ -109,16 +117,15 @@ template <int D>
 __global__ void __launch_bounds__(kCopyThreads) seg4_kernel(const Seg4Args a) {
   constexpr int PPT = D / 8;                               // pieces per token
   constexpr int TT = kCopyThreads * kCopyVecs / PPT;
-  const int64_t g = blockIdx.x;
+  const uint32_t g = blockIdx.x;                           // tiles fit 31 bits
   int i = 0;
   while (i < a.n_segs - 1 && g >= a.tile_end[i]) ++i;
-  const int64_t local = g - (i > 0 ? a.tile_end[i - 1] : 0);
-  const int32_t tpr = a.tiles_per_row[i];
-  const int64_t row = local / tpr;
+  const uint32_t local = g - (i > 0 ? a.tile_end[i - 1] : 0), tpr = a.tiles_per_row[i];
+  const uint32_t row = local / tpr;
   const int32_t tile = (int32_t)(local - row * tpr);
-  const int32_t lh_count = a.n_layers * a.n_kv_heads;
-  const int32_t which = (int32_t)(row / lh_count);         // 0: K, 1: V
-  const int32_t lh = (int32_t)(row - (int64_t)which * lh_count);
+  const uint32_t lh_count = a.n_layers * a.n_kv_heads;
+  const bool which = row >= lh_count;                      // 0: K, 1: V
+  const int32_t lh = (int32_t)(which ? row - lh_count : row);
   const int32_t layer = lh / a.n_kv_heads, h = lh - layer * a.n_kv_heads;
   const int32_t t0 = tile * TT;
   const int32_t n = min(TT, a.len[i] - t0) * PPT;          // pieces of the tile
@@ -163,7 +170,12 @@ __global__ void __launch_bounds__(kCopyThreads) seg4_kernel(const Seg4Args a) {
     } else {
       const int64_t col = ring_add(c0, t, a.cap);
       __builtin_nontemporal_store(code[r], reinterpret_cast<uint32_t*>(dst + col * (D / 2)) + e);
-      if (e % 4 == 0) dst[plane + col * (D / 32) + e / 4] = (uint8_t)scale[r];
+      // a token's scales, one from every fourth of its lanes, in one store
+      const uint32_t all = mx_scales<D>(scale[r]);
+      if (e == 0) {
+        if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst + plane + col * 4) = all;
+        else *reinterpret_cast<uint16_t*>(dst + plane + col * 2) = (uint16_t)all;
+      }
     }
   }
 }

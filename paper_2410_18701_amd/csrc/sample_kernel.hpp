@@ -21,8 +21,8 @@
 // and the latency of its dependent steps, so whole passes over the row are kept few
 // and a list of tokens in LDS takes their place as soon as one can:
 //  * top_k up to 512: the k-th largest of the threads' own largest values bounds
-//    the k-th largest from below; the tokens from there on, a few more than k, are
-//    the list.
+//    the k-th largest from below (up to 1536, counts in bins of the values do); the
+//    tokens from there on, a few more than k, are the list.
 //  * else 1024 bins of equal width over the top of the values' range hold counts
 //    or weights (floats' own bits would put most tokens into a few bins, whose atomics
 //    then queue); a scan finds the bin in which a prefix ends, and that bin's
@@ -45,6 +45,7 @@ constexpr int kSampleBins = 1024;        // == kSampleThreads: a bin per thread
 constexpr int kSampleList = 2048;        // tokens in a list at most, two per thread
 constexpr int kSampleRank = 192;         // up to here a list is ordered by counting, not sorted
 constexpr int kSampleTopK = 512;         // the largest top_k for which threads' largest values bound it
+constexpr int kSampleTopKList = 1536;    // and the largest whose tokens are gathered as a list
 constexpr int kSampleQuarters = 4;       // of the row, with bins of their own
 constexpr int kSampleRowBytes = 80 << 10;    // of a row kept in LDS
 
@@ -627,18 +628,26 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
   const bool want_p = top_p < 1.f;
   uint64_t cut = 0;       // tokens kept: list ids from here on
   uint64_t total;
-  if (want_k && top_k <= kSampleTopK) {
-    // A bin that holds or follows the k-th largest of the threads' largest values: at
-    // least k tokens lie up to it.
-    const float first = p.infinite ? (own == INFINITY ? 1.f : -INFINITY) : own;
-    if (p.valid(first)) atomicAdd(&s.count[p.bin_of(first)], 1u);
+  if (want_k && top_k <= kSampleTopKList) {
+    // A bin up to which at least top_k tokens lie: that of the k-th largest of the
+    // threads' own largest values, or, for a larger k, of the k-th largest of all.
+    if (top_k <= kSampleTopK) {
+      const float first = p.infinite ? (own == INFINITY ? 1.f : -INFINITY) : own;
+      if (p.valid(first)) atomicAdd(&s.count[p.bin_of(first)], 1u);
+    } else {
+      p.each([&](int32_t, const float (&x)[EPV]) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+          if (p.valid(x[e])) atomicAdd(&s.count[p.bin_of(x[e])], 1u);
+      });
+    }
     __syncthreads();
     const uint64_t c = s.count[tid], to = p.wg_scan(c, total);
     if (tid == 0) s.found = kSampleBins;
     __syncthreads();
     if (to >= (uint64_t)top_k && to - c < (uint64_t)top_k) s.found = tid;
     __syncthreads();
-    const int bin = s.found;       // (fewer threads with a valid value than k: every bin)
+    const int bin = s.found;       // (fewer than k counted: every bin)
     s.count[tid] = 0;
     p.collect(fmaxf(p.bin_low(bin), mn), mx, [&](int32_t, int, float x) { return p.bin_of(x) <= bin; });
     const uint32_t n = s.n_list;
