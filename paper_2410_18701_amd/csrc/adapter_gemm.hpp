@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_down_kernel(con
       for (int i = 0; i < U; ++i) {
         const int k = 32 * (s + i);
         const bool in = s + i < s1 && k + 8 * g4 < a.K;   // K is a multiple of 8
-        aw[i] = in ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(ar + k)) : zero;
+        aw[i] = in ? *reinterpret_cast<const u32x4*>(ar + k) : zero;
 #pragma unroll
         for (int t = 0; t < NT; ++t) xw[i][t] = in ? *reinterpret_cast<const u32x4*>(xr[t] + k) : zero;
       }
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
       const uint16_t* br = g.b + (int64_t)col * rank + 8 * g4;
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk)
-        bw[j][kk] = 32 * kk + 8 * g4 < rank ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(br + 32 * kk)) : zero;
+        bw[j][kk] = 32 * kk + 8 * g4 < rank ? *reinterpret_cast<const u32x4*>(br + 32 * kk) : zero;
     }
   };
   // y of the first tile of batch rows at those columns
