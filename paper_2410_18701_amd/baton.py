@@ -297,11 +297,13 @@ def baton_linear_adapters_workspace_bytes(rows, n_parts, max_rank):
 def baton_linear_adapters(dtype, x, adapters, n_adapters, row_adapter, y, rows, out_dim, in_dim, part_dims, n_parts,
                           accumulate, ws, ws_bytes, stream=None):
     """adapters: a ctypes array of baton_adapter (or None); row_adapter: rows integers;
-    part_dims: n_parts integers or None."""
+    part_dims: n_parts integers, a ctypes array of them, or None."""
     ids = (ctypes.c_int32 * max(1, len(row_adapter)))(*row_adapter)
     if len(row_adapter) != rows or (part_dims is not None and len(part_dims) != n_parts):
         raise ValueError("row_adapter needs an entry per row, part_dims one per part")
-    parts = None if part_dims is None else (ctypes.c_int32 * max(1, n_parts))(*part_dims)
+    parts = part_dims
+    if parts is not None and not isinstance(parts, ctypes.Array):
+        parts = (ctypes.c_int32 * max(1, n_parts))(*parts)
     _check(lib().baton_linear_adapters(dtype, _ptr(x), adapters, n_adapters, ids, _ptr(y), rows, out_dim, in_dim,
                                        parts, n_parts, int(accumulate), _ptr(ws), ws_bytes, _stream(stream)),
            "baton_linear_adapters")

@@ -1,6 +1,7 @@
 // Low-rank adapters of many requests beside a shared projection:
 //   y[r] (+)= scale_g * (x[r] . A_g^T) . B_g^T,  g the adapter of row r,
-// in two launches over the rows sorted by adapter.  What bounds both is reading
+// in two launches over the rows sorted by adapter (in one where both are short,
+// adapter_small_kernel).  What bounds both is reading
 // the adapters' weights once (and, for a few small ones, the launches' latency):
 // a batch of 64 rows over 24 adapters does 1 to 3 flops per byte.
 //  * down: h = x . A^T, [rows][parts * rank].  A workgroup takes 16 of an
@@ -55,6 +56,12 @@ struct AdapterArgs {
   uint16_t row[kAdapterMaxRows];   // sorted place -> batch row
 };
 static_assert(sizeof(AdapterArgs) <= 4096, "kernel arguments");
+
+// f as two bf16 halves; nothing remains of what rounds to an infinity (or is one, or a NaN).
+__device__ __forceinline__ void adapter_split(float f, uint32_t& hi, uint32_t& lo) {
+  hi = f32_to_bf16_rne(f);
+  lo = (hi & 0x7F80u) == 0x7F80u ? 0u : f32_to_bf16_rne(f - __uint_as_float(hi << 16));
+}
 
 __device__ __forceinline__ ad_bf16x8 ad_vec(const u32x4& w) { return __builtin_bit_cast(ad_bf16x8, w); }
 
@@ -131,6 +138,23 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_down_kernel(con
     *reinterpret_cast<ad_f32x4*>(a.h + ((int64_t)split * a.rows + first + r) * a.hs + j) = sum;
 }
 
+// Workgroup `local` of a group's row blocks rb x columns, taken part by part, `wide` at
+// a time: its part p and first column c0; c_end is the part's end.
+__device__ __forceinline__ void adapter_columns(const AdapterArgs& a, int local, int wide, int& rb, int& p, int& c0,
+                                                int& c_end) {
+  int per_rb = 0;
+  for (int q = 0; q < a.parts; ++q) per_rb += (a.part_end[q] - (q > 0 ? a.part_end[q - 1] : 0) + wide - 1) / wide;
+  rb = local / per_rb;
+  int chunk = local - rb * per_rb;
+  for (p = 0;; ++p) {
+    const int b0 = p > 0 ? a.part_end[p - 1] : 0, cnt = (a.part_end[p] - b0 + wide - 1) / wide;
+    c0 = b0 + chunk * wide;
+    c_end = a.part_end[p];
+    if (chunk < cnt || p == a.parts - 1) return;
+    chunk -= cnt;
+  }
+}
+
 // Elements between two staged rows of h, of NKK 32-wide steps: padded by 16 bytes.
 template <int NKK>
 constexpr int adapter_row() { return 32 * NKK + 8; }
@@ -145,22 +169,8 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
   const int gi = adapter_group<true>(a, blockIdx.x);
   const AdapterGroup& g = a.g[gi];
   const int local = (int)blockIdx.x - (gi > 0 ? a.g[gi - 1].up_end : 0);
-  // the workgroup's columns: part by part, kAdapterWaves * cols at a time
-  int per_rb = 0, p = 0, c0 = 0, c_end = 0;
-  const int wide = kAdapterWaves * a.cols;
-  for (int q = 0; q < a.parts; ++q) per_rb += (a.part_end[q] - (q > 0 ? a.part_end[q - 1] : 0) + wide - 1) / wide;
-  const int rb = local / per_rb;
-  int chunk = local - rb * per_rb;
-  for (int q = 0; q < a.parts; ++q) {
-    const int b0 = q > 0 ? a.part_end[q - 1] : 0, cnt = (a.part_end[q] - b0 + wide - 1) / wide;
-    if (chunk < cnt) {
-      p = q;
-      c0 = b0 + chunk * wide;
-      c_end = a.part_end[q];
-      break;
-    }
-    chunk -= cnt;
-  }
+  int rb, p, c0, c_end;
+  adapter_columns(a, local, kAdapterWaves * a.cols, rb, p, c0, c_end);
   const int first = g.begin + rb * kAdapterRows;
   const int n = min((gi + 1 < a.n_groups ? a.g[gi + 1].begin : a.end) - first, kAdapterRows);
   const int rank = g.rank, n_rt = (n + 15) / 16;
@@ -202,12 +212,7 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
     }
     uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float f = v[e] * g.scale;
-      hi[e] = f32_to_bf16_rne(f);
-      // nothing remains of what rounds to an infinity (or is one, or a NaN)
-      lo[e] = (hi[e] & 0x7F80u) == 0x7F80u ? 0u : f32_to_bf16_rne(f - __uint_as_float(hi[e] << 16));
-    }
+    for (int e = 0; e < 4; ++e) adapter_split(v[e] * g.scale, hi[e], lo[e]);
     *reinterpret_cast<uint2*>(hs_hi + r * ROW + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
     *reinterpret_cast<uint2*>(hs_lo + r * ROW + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
   }
@@ -247,6 +252,100 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
       for (int kk = 0; kk < NKK; ++kk) bw[j][kk] = next[j][kk];
     old = next_old;
   }
+}
+
+// Both products in one launch, for calls of few small adapters, where the launches
+// are the time: up to 16 rows and rank 32 a group.  Every workgroup forms the whole h
+// of its part -- its 16 waves divide k and add through LDS -- for 512 columns of y, so
+// A is read from the caches once for each 512 columns.
+constexpr int kAdapterSmallWaves = 16, kAdapterSmallRank = 32, kAdapterSmallRows = 16;
+constexpr int kAdapterSmallCols = 32 * kAdapterSmallWaves;
+
+// AT = 16-row tiles of A: ranks up to 16 or 32.
+template <int AT>
+__global__ void __launch_bounds__(kWave * kAdapterSmallWaves) adapter_small_kernel(const AdapterArgs a) {
+  constexpr int NW = kAdapterSmallWaves, ROW = adapter_row<1>(), U = 8 / AT;   // U steps' loads in flight
+  __shared__ ad_f32x4 part[NW][AT][kWave];
+  __shared__ __attribute__((aligned(16))) uint16_t hs_hi[16 * ROW], hs_lo[16 * ROW];
+  const int gi = adapter_group<true>(a, blockIdx.x);
+  const AdapterGroup& g = a.g[gi];
+  const int local = (int)blockIdx.x - (gi > 0 ? a.g[gi - 1].up_end : 0);
+  int rb, p, c0, c_end;
+  adapter_columns(a, local, kAdapterSmallCols, rb, p, c0, c_end);   // rb = 0
+  const int first = g.begin, n = (gi + 1 < a.n_groups ? a.g[gi + 1].begin : a.end) - first;
+  const int rank = g.rank;
+  const int tid = threadIdx.x, lane = tid % kWave, g4 = lane / 16, c16 = lane % 16;
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const u32x4 zero = {0, 0, 0, 0};
+  const int row = a.row[first + min(c16, n - 1)];     // rows past the last read it again
+  // this wave's 32 columns of B and y, on their way while h is formed
+  const int c = c0 + 32 * w;
+  const bool ok = c16 < n && c + 8 * g4 < c_end;
+  u32x4* const yp = reinterpret_cast<u32x4*>(a.y + (int64_t)row * a.N + c + 8 * g4);
+  u32x4 bw[2], old = zero;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int col = min(c + 8 * (c16 / 4) + 4 * j + c16 % 4, c_end - 1);
+    bw[j] = 8 * g4 < rank ? *reinterpret_cast<const u32x4*>(g.b + (int64_t)col * rank + 8 * g4) : zero;
+  }
+  if (ok && a.accumulate) old = *yp;
+  const int steps = rank > 0 ? (a.K + 31) / 32 : 0, per = (steps + NW - 1) / NW;
+  const int s0 = w * per, s1 = min(s0 + per, steps);
+  const uint16_t* xr = a.x + (int64_t)row * a.K + 8 * g4;
+  const uint16_t* ar[AT];
+#pragma unroll
+  for (int t = 0; t < AT; ++t)
+    ar[t] = g.a + ((int64_t)p * rank + max(min(16 * t + c16, rank - 1), 0)) * a.K + 8 * g4;
+  ad_f32x4 acc[AT];
+#pragma unroll
+  for (int t = 0; t < AT; ++t) acc[t] = ad_f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s = s0; s < s1; s += U) {
+    u32x4 xw[U], aw[U][AT];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int k = 32 * (s + i);
+      const bool in = s + i < s1 && k + 8 * g4 < a.K;
+      xw[i] = in ? *reinterpret_cast<const u32x4*>(xr + k) : zero;
+#pragma unroll
+      for (int t = 0; t < AT; ++t) aw[i][t] = in ? *reinterpret_cast<const u32x4*>(ar[t] + k) : zero;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int t = 0; t < AT; ++t)
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(aw[i][t]), ad_vec(xw[i]), acc[t], 0, 0, 0);
+  }
+#pragma unroll
+  for (int t = 0; t < AT; ++t) part[w][t][lane] = acc[t];
+  __syncthreads();
+  if (w < 2) {     // wave t: 4 ranks from 16 t + 4 (l / 16) on of batch row l % 16
+    ad_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (w < AT) {
+#pragma unroll
+      for (int q = 0; q < NW; ++q) v += part[q][w][lane];
+    }
+    const int j = 16 * w + 4 * g4;
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) adapter_split(c16 < n && j < rank ? v[e] * g.scale : 0.f, hi[e], lo[e]);
+    *reinterpret_cast<uint2*>(hs_hi + c16 * ROW + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+    *reinterpret_cast<uint2*>(hs_lo + c16 * ROW + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+  }
+  __syncthreads();
+  const ad_bf16x8 hi = ad_vec(*reinterpret_cast<const u32x4*>(hs_hi + c16 * ROW + 8 * g4));
+  const ad_bf16x8 lo = ad_vec(*reinterpret_cast<const u32x4*>(hs_lo + c16 * ROW + 8 * g4));
+  u32x4 o;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    ad_f32x4 d = {0.f, 0.f, 0.f, 0.f};
+    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j]), lo, d, 0, 0, 0);
+    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j]), hi, d, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      o[2 * j + e] = f32_to_bf16_rne(bf16_lo(old[2 * j + e]) + d[2 * e]) |
+                     f32_to_bf16_rne(bf16_hi(old[2 * j + e]) + d[2 * e + 1]) << 16;
+  }
+  if (ok) *yp = o;
 }
 
 }  // namespace

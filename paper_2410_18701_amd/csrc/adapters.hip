@@ -101,6 +101,24 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
       units += (int64_t)rbs * ((n_parts * g.rank + 15) / 16);
     }
     a.end = (int16_t)at;
+    const dim3 block(kWave * kAdapterWaves);
+    int32_t small = 0;     // workgroups of the single launch for each row block
+    for (int32_t p = 0; p < n_parts; ++p)
+      small += (a.part_end[p] - (p > 0 ? a.part_end[p - 1] : 0) + kAdapterSmallCols - 1) / kAdapterSmallCols;
+    // One launch while a part's A is up to 128 KB, which each workgroup reads, and the
+    // workgroups make one round.  us by both, calls from Python: one row of rank 16,
+    // 4096 to 4096 8.7 / 10.4, 11008 to 4096 16.2 / 10.1; 32 adapters of rank 8, 2048 to
+    // 2048 8.0 / 11.1; of rank 16, 4096 to 4096: 8 9.3 / 10.0, 32 (256 workgroups) 10.8 /
+    // 11.2, 64 19.2 / 12.0.
+    if (max_rank <= kAdapterSmallRank && lds_rows <= kAdapterSmallRows && (int64_t)max_rank * in_dim <= 1 << 16 &&
+        (int64_t)a.n_groups * small <= 256) {
+      for (int32_t i = 0; i < a.n_groups; ++i) a.g[i].up_end = (i + 1) * small;
+      const dim3 grid((unsigned)(a.n_groups * small)), wide(kWave * kAdapterSmallWaves);
+      if (max_rank <= 16) hipLaunchKernelGGL(adapter_small_kernel<1>, grid, wide, 0, stream, a);
+      else hipLaunchKernelGGL(adapter_small_kernel<2>, grid, wide, 0, stream, a);
+      if (hipGetLastError() != hipSuccess) return BATON_EHIP;
+      continue;
+    }
     // Ranges of k: about 1024 workgroups in all, at least eight steps of 32 (the
     // loads a wave has in flight at once) for each wave.  us of both launches, 256
     // rows of 40 adapters of rank 64, 4096 to 2 x 11008: 50.2, with 512 workgroups 53.7;
@@ -127,7 +145,6 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
       g.down_end = (int32_t)down;
       g.up_end = (int32_t)up;
     }
-    const dim3 block(kWave * kAdapterWaves);
     if (down > 0) hipLaunchKernelGGL(adapter_down_kernel, dim3((unsigned)down), block, 0, stream, a);
     auto launch_up = [&](auto kernel, int32_t row) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)up), block, (size_t)lds_rows * row * 2 * sizeof(uint16_t), stream, a, lds_rows);

@@ -9,6 +9,8 @@ projection -> silu(gate) * up -> down projection added to the residual stream.
 What each query of the batch brings of its own joins it: low-rank adapters
 beside the projections, and its sampling parameters for the next token.
 """
+import ctypes
+
 from . import baton as B
 from .cache import _cur_stream as _stream
 
@@ -31,7 +33,7 @@ class Adapters:
         if not len(a) == len(b) == len(scales):
             raise ValueError("Adapters: a, b and scales need the same length")
         self.a, self.b, self.n = list(a), list(b), len(a)
-        self.parts = None if parts is None else [int(p) for p in parts]
+        self.parts = None if parts is None else (ctypes.c_int32 * len(parts))(*[int(p) for p in parts])
         n_parts = 1 if parts is None else len(self.parts)
         self.max_rank = max((t.shape[1] for t in self.b), default=0)
         self.table = (B.baton_adapter * max(1, self.n))()
