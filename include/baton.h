@@ -569,7 +569,7 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
  * (45 at a vocabulary of 128,000), sums in any order alike, so the same inputs
  * give the same token.
  * logits aligned to their element; the arrays to 4 bytes.
- * Errors: EINVAL (null logits, u or tokens, rows < 1, vocab outside 1..2^24,
+ * Errors: EINVAL (null logits, u or tokens, rows outside 1..2^21, vocab outside 1..2^24,
  * ld < vocab, misaligned pointer), EDTYPE, EHIP.
  */
 baton_status baton_sample(int32_t dtype, const void* logits, int64_t ld, int32_t rows, int32_t vocab,

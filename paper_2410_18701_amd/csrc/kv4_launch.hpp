@@ -8,6 +8,19 @@
 
 bool is_kv4(const baton_cache* c) { return c->d.dtype == BATON_MXFP4; }
 
+// The tiles of a's segments, kSeg4Tiles to a launch.
+template <int D>
+baton_status launch_tiles4(baton::Seg4Args& a, int64_t tiles, hipStream_t s) {
+  if (tiles > 0x7FFFFFFF) return BATON_EINVAL;
+  for (a.tile0 = 0; a.tile0 < tiles; a.tile0 += baton::kSeg4Tiles) {
+    const uint32_t n = std::min(baton::kSeg4Tiles, (uint32_t)tiles - a.tile0);
+    hipLaunchKernelGGL(baton::seg4_kernel<D>, dim3(n), dim3(baton::kCopyThreads), 0, s, a);
+    const baton_status st = hip_status(hipGetLastError());
+    if (st != BATON_OK) return st;
+  }
+  return BATON_OK;
+}
+
 template <int D>
 baton_status launch_segs4_d(const baton_cache* c, const std::vector<Seg>& segs, int mode, hipStream_t s) {
   constexpr int PPT = D / 8, TT = baton::kCopyThreads * baton::kCopyVecs / PPT;
@@ -45,10 +58,7 @@ baton_status launch_segs4_d(const baton_cache* c, const std::vector<Seg>& segs, 
       ++used;
     }
     a.n_segs = used;
-    if (used == 0) continue;
-    if (tiles > 0x7FFFFFFF) return BATON_EINVAL;
-    hipLaunchKernelGGL(baton::seg4_kernel<D>, dim3((unsigned)tiles), dim3(baton::kCopyThreads), 0, s, a);
-    const baton_status st = hip_status(hipGetLastError());
+    const baton_status st = launch_tiles4<D>(a, tiles, s);
     if (st != BATON_OK) return st;
   }
   return BATON_OK;
@@ -90,9 +100,7 @@ baton_status append_prompts4_d(const baton_cache* c, const baton::PrefillArgs& p
       tiles += (int64_t)a.tiles_per_row[i] * 2 * p.n_kv_heads;
       a.tile_end[i] = (uint32_t)tiles;
     }
-    if (tiles > 0x7FFFFFFF) return BATON_EINVAL;
-    hipLaunchKernelGGL(baton::seg4_kernel<D>, dim3((unsigned)tiles), dim3(baton::kCopyThreads), 0, s, a);
-    const baton_status st = hip_status(hipGetLastError());
+    const baton_status st = launch_tiles4<D>(a, tiles, s);
     if (st != BATON_OK) return st;
   }
   return BATON_OK;

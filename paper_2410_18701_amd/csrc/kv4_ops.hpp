@@ -86,6 +86,9 @@ __device__ __forceinline__ uint32_t mx_scales(uint32_t s) {
   return s;
 }
 
+// Tiles (workgroups) of a launch: some 4 GB of sources, far below 2^32 threads.
+constexpr uint32_t kSeg4Tiles = 1u << 18;
+
 // SegArgs for a 4-bit ring: segments as there, the contiguous side in bf16 with
 // its own strides (a prompt's keys lie [position][head][D], a prefilled query's
 // [layer][head][position][D]).  k, v and layer_vec as in SegArgs.
@@ -96,6 +99,7 @@ struct Seg4Args {
   int64_t layer_bytes;      // from one layer's rows to the next layer's
   int32_t n_layers, batch, n_kv_heads;
   int32_t n_segs;
+  uint32_t tile0;           // tile of the launch's first workgroup
   int32_t mode;             // 0: ext (or placeholder) -> ring, 1: ring -> ext, 2: ring row -> ring row
   uint32_t fill_word;       // placeholder byte, four times
   int32_t slot[kMaxSegs];
@@ -117,7 +121,7 @@ template <int D>
 __global__ void __launch_bounds__(kCopyThreads) seg4_kernel(const Seg4Args a) {
   constexpr int PPT = D / 8;                               // pieces per token
   constexpr int TT = kCopyThreads * kCopyVecs / PPT;
-  const uint32_t g = blockIdx.x;                           // tiles fit 31 bits
+  const uint32_t g = a.tile0 + blockIdx.x;                 // tiles fit 31 bits
   int i = 0;
   while (i < a.n_segs - 1 && g >= a.tile_end[i]) ++i;
   const uint32_t local = g - (i > 0 ? a.tile_end[i - 1] : 0), tpr = a.tiles_per_row[i];

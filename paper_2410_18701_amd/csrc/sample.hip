@@ -28,7 +28,8 @@ extern "C" {
 baton_status baton_sample(int32_t dtype, const void* logits, int64_t ld, int32_t rows, int32_t vocab,
                           const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                           const float* u, int32_t* tokens, hipStream_t stream) {
-  if (!logits || !u || !tokens || rows < 1 || vocab < 1 || vocab > (1 << 24) || ld < vocab || ld > (int64_t(1) << 40))
+  // fewer than 2^32 threads: 1024 a row
+  if (!logits || !u || !tokens || rows < 1 || rows > (1 << 21) || vocab < 1 || vocab > (1 << 24) || ld < vocab || ld > (int64_t(1) << 40))
     return BATON_EINVAL;
   if (dtype != BATON_F32 && dtype != BATON_BF16) return BATON_EDTYPE;
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == BATON_F32 ? 4 : 2) || !aligned4(temperature) ||

@@ -15,6 +15,15 @@ from . import baton as B
 from .cache import _cur_stream as _stream
 
 
+def _on_this_gpu(what, *tensors):
+    """The calls go to the current device's stream: tensors elsewhere are refused."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"{what}: a tensor on {t.device}, the current device is cuda:{here}")
+
+
 class PackedWeight:
     """A weight in the packed form baton_linear_packed reads."""
 
@@ -111,13 +120,15 @@ class Gemm:
     def linear_adapters(self, x, adapters, row_adapter, y, accumulate=False):
         """y (+)= each row's low-rank product with its adapter: x [rows <= 256][in], y [rows][out],
         row_adapter a list of rows indices into adapters (-1: none)."""
+        import torch
         rows, in_dim = x.shape
         if y.shape[0] != rows or y.dim() != 2 or len(row_adapter) != rows or \
                 (adapters.n and (in_dim != adapters.in_dim or y.shape[1] != adapters.out_dim)):
             raise ValueError("linear_adapters: shapes do not match")
         for t in (x, y):
-            if not t.is_contiguous():
-                raise ValueError("linear_adapters: contiguous tensors only")
+            if not t.is_contiguous() or t.dtype != torch.bfloat16:
+                raise ValueError("linear_adapters: contiguous bf16 tensors only")
+        _on_this_gpu("linear_adapters", x, y, *adapters.a[:1])
         B.baton_linear_adapters(B.BATON_BF16, x, adapters.table, adapters.n, row_adapter, y, rows, y.shape[1], in_dim,
                                 adapters.parts, 1 if adapters.parts is None else len(adapters.parts), accumulate,
                                 self.ws, self.ws_bytes, _stream())
@@ -178,6 +189,7 @@ class Sampler:
                 continue
             if t.dtype != want or t.numel() != self.rows or not t.is_contiguous():
                 raise ValueError(f"Sampler: {name} must be {self.rows} contiguous {want} values")
+        _on_this_gpu("Sampler", self.tokens, logits, u, temperature, top_k, top_p, min_p)
         ld = logits.stride(0) if self.rows > 1 else self.vocab
         B.baton_sample(dtype, logits, ld, self.rows, self.vocab, temperature, top_k, top_p, min_p, u, self.tokens,
                        _stream())

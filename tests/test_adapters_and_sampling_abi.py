@@ -80,6 +80,7 @@ def sample_status(dtype=B.BATON_BF16, logits=X, ld=100, rows=4, vocab=100, tempe
 
 @pytest.mark.parametrize("kw", [
     dict(logits=0), dict(logits=X + 1), dict(dtype=B.BATON_F32, logits=X + 2), dict(ld=99), dict(rows=0), dict(rows=-1),
+    dict(rows=(1 << 21) + 1),
     dict(vocab=0), dict(vocab=(1 << 24) + 1, ld=1 << 25), dict(u=0), dict(u=W + 2), dict(tokens=0), dict(tokens=Y + 1),
     dict(temperature=A + 2), dict(top_k=A + 1), dict(top_p=A + 3), dict(min_p=A + 2), dict(ld=(1 << 40) + 1),
 ], ids=lambda kw: "-".join(kw))

@@ -186,6 +186,9 @@ def test_story(shape, layout):
     p.step()
     p.step(prompts={})
     p.evict([0, 4], scrub=True)
+    p.move([3], [0])                    # a row with holes, over owed placeholders
+    p.step()
+    p.move([0], [3])
     p.step(prompts={0: 1})
     p.step(prompts={4: 70})
     for _ in range(2):
@@ -241,6 +244,23 @@ def test_a_stored_nan_reaches_its_row_alone():
     assert out[0, 1].all() and not out[0, 0].any()
     assert out[1, 0, 32:64].all() and not out[1, 0, :32].any() and not out[1, 0, 64:].any() and not out[1, 1].any()
     assert not out[2].any()
+
+
+def test_more_tiles_than_one_launch():
+    """32 queries of one to three tokens over 128 layers of 64 heads: 524,288 tiles to an embed."""
+    layers, slots, heads, d = 128, 32, 64, 64
+    c = BatonCache(layers, slots, heads, heads, d, 16, dtype="mxfp4")
+    lens = [1 + b % 3 for b in range(slots)]
+    ks, vs = ([torch.randn(layers, heads, n, d, device="cuda").bfloat16() for n in lens] for _ in range(2))
+    c.embed(list(range(slots)), lens, ks, vs)
+    gk, gv = c.extract(list(range(slots)))
+    for b in (0, 1, 30, 31):
+        for got, src in ((gk[b], ks[b]), (gv[b], vs[b])):
+            for l in (0, 77, 127):
+                assert np.array_equal(val(got[l]), X.stored(val(src[l])))
+    again = BatonCache(layers, slots, heads, heads, d, 16, dtype="mxfp4")
+    again.embed(list(range(slots)), lens, gk, gv)
+    assert torch.equal(c.k, again.k) and torch.equal(c.v, again.v)
 
 
 def test_placeholders():
