@@ -43,7 +43,7 @@ namespace {
 constexpr int kSampleThreads = 1024, kSampleWaves = kSampleThreads / kWave;
 constexpr int kSampleBins = 1024;        // == kSampleThreads: a bin per thread
 constexpr int kSampleList = 2048;        // tokens in a list at most, two per thread
-constexpr int kSampleRank = 192;         // up to here a list is ordered by counting, not sorted
+constexpr int kSampleRank = 256;         // up to here a list is ordered by counting, not sorted
 constexpr int kSampleTopK = 512;         // the largest top_k for which threads' largest values bound it
 constexpr int kSampleTopKList = 1536;    // and the largest whose tokens are gathered as a list
 constexpr int kSampleQuarters = 4;       // of the row, with bins of their own
@@ -143,6 +143,8 @@ struct SampleShared {
   uint32_t count[kSampleBins];
   uint64_t list[kSampleList];    // tokens: (float_key, ~index), so that larger is earlier
   uint64_t lw[kSampleList];      // their weights
+  uint64_t ahead_w[kSampleRank];
+  uint32_t ahead[kSampleRank];
   uint64_t scan[2][kSampleWaves];
   uint64_t part[kSampleWaves], quarter[kSampleQuarters];
   float fmax[kSampleWaves], fmin[kSampleWaves];
@@ -324,25 +326,43 @@ struct Sampler {
       p[0].before_w = p[1].before_w - p[0].w;
       return;
     }
+    // Token e against a quarter of the list in each of four threads.
+    const uint32_t e = tid % kSampleRank, q = tid / kSampleRank;
+    static_assert(kSampleThreads == 4 * kSampleRank, "four threads per token");
+    const bool in = e < n;
+    const uint64_t id = in ? s.list[e] : 0;
+    uint64_t g = 0;
+    if (q == 0) {
+      g = weight_of(key_float((uint32_t)(id >> 32)));
+      g = in ? g : 0;
+      s.lw[e] = g;
+      s.ahead[e] = 0;
+      s.ahead_w[e] = 0;
+    }
+    __syncthreads();
+    const uint32_t j0 = q * n / 4, j1 = (q + 1) * n / 4;
+    uint64_t bw = 0;
+    uint32_t b = 0;
+    if (w % 4 * kWave < n) {
+#pragma unroll 4
+      for (uint32_t j = j0; j < j1; ++j) {
+        const uint64_t other = s.list[j], ow = s.lw[j];
+        const bool first = other > id;
+        b += first;
+        bw += first ? ow : 0;
+      }
+      atomicAdd(&s.ahead[e], b);
+      atomicAdd(reinterpret_cast<unsigned long long*>(&s.ahead_w[e]), (unsigned long long)bw);
+    }
+    __syncthreads();
+    p[0].in = q == 0 && in;
+    p[0].id = q == 0 ? id : 0;
+    p[0].w = g;
+    p[0].before = s.ahead[e];
+    p[0].before_w = s.ahead_w[e];
     p[1].in = false;
     p[1].w = p[1].before_w = p[1].id = 0;
     p[1].before = 0;
-    p[0].in = (uint32_t)tid < n;
-    p[0].id = p[0].in ? s.list[tid] : 0;
-    const uint64_t g = weight_of(key_float((uint32_t)(p[0].id >> 32)));
-    p[0].w = p[0].in ? g : 0;
-    if (p[0].in) s.lw[tid] = g;
-    __syncthreads();
-    uint64_t bw = 0;
-    uint32_t b = 0;
-    if ((uint32_t)(w * kWave) < n)
-      for (uint32_t j = 0; j < n; ++j) {
-        const bool ahead = s.list[j] > p[0].id;
-        b += ahead;
-        bw += ahead ? s.lw[j] : 0;
-      }
-    p[0].before = b;
-    p[0].before_w = bw;
   }
 
   __device__ __forceinline__ int quarter_of(uint32_t index) const {
