@@ -3,9 +3,12 @@
 // merge are those of the bf16 kernels.
 //
 // What bounds it is HBM -- 68 bytes of K or V per token at head_dim 128, against
-// 256 in bf16 -- as long as turning codes into operands costs few instructions:
-// a wave that streams its share of 8 TB/s has about 40 vector instructions per
-// token row pair and 64 lanes.  Per iteration a wave takes 64 tokens:
+// 256 in bf16 -- as long as turning codes into operands costs few instructions,
+// and then each item's start (its descriptor, the query, the first loads) and end:
+// 37 us for 152 MB (32 rows of up to 2048 tokens, 32 heads; 4.1 TB/s), 59 for 295 MB
+// (61 rows of up to 8192, 64 heads over 8; 5.0), where a copy of it that only loads
+// takes 32 and 54 and a plain read of as many bytes 23 and 42.  The vector ALUs are
+// active 49% of the time, the matrix cores 12%.  Per iteration a wave takes 64 tokens:
 //  * QK^T: A = 16 key rows x 32 of d, four tiles of 16 consecutive tokens.  The
 //    contraction's order is free, so lane l takes the D / 4 elements from D / 4 *
 //    (l / 16) on of its key row -- one load of 16 bytes (8 at head_dim 64), a
@@ -26,8 +29,10 @@
 //    REP = min(D / 32, 16 / G) columns per head each carry another block, and of the
 //    16 result columns only the one with the slice's block is kept (at G = 8 and
 //    head_dim 128 two blocks share a column and P' is formed twice).
-// Weights are rounded to bf16 for the product (half a step, 2^-9 of each); their sum
-// is taken in fp32 before that rounding.
+// Weights are rounded to bf16 for the product (at most 2^-8 of each); their sum is
+// taken in fp32 before that rounding.
+// Registers are capped for three waves per SIMD (166 used); for four they spill, and
+// the kernel takes 1.5 to 2 times as long.
 // The step's own key and value take part as given, in bf16, and are stored in 4 bits.
 #pragma once
 

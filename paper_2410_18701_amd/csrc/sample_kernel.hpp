@@ -9,7 +9,7 @@
 //
 // A result is an index, so weights and sums have to be the same whatever the order
 // they are formed in, and near those of 64-bit arithmetic: a weight is
-// computed in double precision (relative error about 2^-52) and rounded to a whole
+// computed in double precision (relative error below 2^-49) and rounded to a whole
 // number of 2^-shift, shift = 62 - ceil(log2 V) at most 51.  Sums of whole numbers are
 // exact, so atomics in any order give the same sums, and the boundary between two
 // tokens is off by about sqrt(V) 2^-(shift + 1) at most.
@@ -33,6 +33,9 @@
 //    weights per wave, then the tokens of the wave's part in which the target lies.
 // exp: 2^(j / 128) from a table, times a polynomial of degree 4 on half a step:
 // relative error below 2^-49.
+// us, bf16: one row of 32,000 8 (greedy), 13 (top_k 50), 15 (temperature alone), 23 to
+// 26 (top_p); 256 rows of 128,000, which LDS holds a third of, 25, 32, 49 and 80 to 88,
+// of which 13.5 is the first read and 36 the bins' weights.
 #pragma once
 
 #include "common.hpp"
