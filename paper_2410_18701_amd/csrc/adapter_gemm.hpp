@@ -17,7 +17,7 @@
 //    h would be rounded to 8 bits.
 // Sums are fp32 in a fixed order: the same call gives the same bits.
 // us down / up: 64 rows of 24 adapters of rank 32, 4096 to 3 parts of 4096 (35 MB)
-// 7.0 / 8.2; 240 rows of 40 of rank 64, 4096 to 2 of 11008 (177 MB with y) 15.4 / 36.
+// 7.0 / 8.2; 240 rows of 40 of rank 64, 4096 to 2 of 11008 (177 MB with y) 15.4 / 32.7.
 #pragma once
 
 #include <type_traits>

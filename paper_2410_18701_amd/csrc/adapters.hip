@@ -119,19 +119,20 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
       if (hipGetLastError() != hipSuccess) return BATON_EHIP;
       continue;
     }
-    // Ranges of k: about 1024 workgroups in all, at least eight steps of 32 (the
-    // loads a wave has in flight at once) for each wave.  us of both launches, 256
-    // rows of 40 adapters of rank 64, 4096 to 2 x 11008: 50.2, with 512 workgroups 53.7;
-    // 64 rows of 24 of rank 32, 4096 to 12288: 15.3, with four steps a wave 16.3.
+    // Ranges of k: 1024 workgroups in all or a few more, at least eight steps of 32
+    // (the loads a wave has in flight at once) for each wave.  us of both launches, 256
+    // rows of 40 adapters of rank 64, 4096 to 2 x 11008: with 512 workgroups 53.7, with
+    // 1024 50.2; 64 rows of 24 of rank 32, 4096 to 12288: 15.3, with four steps a wave 16.3.
     const int64_t fit = per_split ? (int64_t)(ws_bytes / per_split) : 1;
-    int64_t splits = units > 0 ? 1024 / units : 1;
+    int64_t splits = units > 0 ? (1024 + units - 1) / units : 1;
     splits = std::max<int64_t>(1, std::min({splits, (int64_t)(steps + 31) / 32, fit, (int64_t)64}));
     a.kt = (int32_t)((steps + splits - 1) / splits);
     a.splits = (steps + a.kt - 1) / a.kt;
-    // Columns of y per wave: about 4096 waves in all, 32 to 256 columns.
+    // Columns of y per wave: about 4096 waves in all, 32 to 128 columns (the first of
+    // those cases with up to 256 49.2, 128 44.4, 64 44.6).
     int64_t rbs = 0;
     for (int32_t i = 0; i < a.n_groups; ++i) rbs += a.g[i].up_end;
-    a.cols = (int32_t)std::max<int64_t>(32, std::min<int64_t>(256, (rbs * out_dim / 4096 + 31) / 32 * 32));
+    a.cols = (int32_t)std::max<int64_t>(32, std::min<int64_t>(128, (rbs * out_dim / 4096 + 31) / 32 * 32));
     int32_t per_rb = 0;
     const int32_t wide = kAdapterWaves * a.cols;
     for (int32_t p = 0; p < n_parts; ++p)

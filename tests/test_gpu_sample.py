@@ -83,6 +83,21 @@ def test_crowded_bins(dtype):
           top_k=rng.choice([0, 3, 2500, 20000], rows).tolist(), top_p=rng.choice([0.1, 0.5, 0.99, 1.0], rows).tolist())
 
 
+def test_many_neighbours_of_a_large_vocabulary():
+    """More kept tokens side by side than one range of the list's draw takes."""
+    vocab, n = 1 << 21, 1500
+    l = np.full((3, vocab), -np.inf, np.float32)
+    rng = np.random.default_rng(8)
+    for r, first in enumerate((0, 4096, vocab - n)):
+        l[r, first:first + n] = rng.standard_normal(n)
+    l[1, 5] = 0.0
+    logits = torch.from_numpy(l).cuda()
+    for u in (0.0, 0.25, 0.5, 0.999999):
+        check(logits, [u] * 3, min_p=[1e-6] * 3)
+        check(logits, [u] * 3, top_k=[1200] * 3)
+        check(logits, [u] * 3, top_p=[0.97] * 3)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_masked_and_infinite_logits(dtype):
     inf, low = float("inf"), -3.3895313892515355e38
@@ -111,6 +126,8 @@ def test_masked_and_infinite_logits(dtype):
         check(logits, [u] * n)
         check(logits, [u] * n, temperature=[0.5] * n, top_k=[30] * n, top_p=[0.9] * n, min_p=[0.01] * n)
         check(logits, [u] * n, temperature=[1e-30] * n, top_k=[2] * n)
+        check(logits, [u] * n, temperature=[0.0] * n)
+        check(logits, [u] * n, top_k=[1000] * n, min_p=[1.0] * n)
         check(logits, [u] * n, temperature=[float("inf")] * n, top_p=[0.5] * n)
     assert run(logits, [0.5] * n)[:2] == [-1, -1]
 
