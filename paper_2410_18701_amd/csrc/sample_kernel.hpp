@@ -619,6 +619,9 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
     mx = fmaxf(mx, s.fmax[v]);
     mn = fminf(mn, s.fmin[v]);
   }
+  // the same in every lane, which the compiler cannot see
+  mx = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(mx)));
+  mn = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(mn)));
   if (mx == -INFINITY) {      // no token can be drawn
     if (tid == 0) a.tokens[r] = -1;
     return;
