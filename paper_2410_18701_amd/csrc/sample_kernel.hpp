@@ -585,17 +585,30 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
 
   // The row into LDS; its largest value and the smallest that is finite.
   float mx = -INFINITY, mn = INFINITY;
-  for (int32_t i0 = p.v0; i0 < p.v1; i0 += kWave) {
-    const int32_t i = i0 + lane;
-    if (i >= p.v1) continue;
-    const u32x4 v = row.fetch(i);
+  auto take = [&](int32_t i, const u32x4& v, bool all) {
     if (i < row.n_lds) row.lds[i] = v;
     float x[EPV];
-    row.widen(i, v, row.inside(i0), x);
+    row.widen(i, v, all, x);
 #pragma unroll
     for (int e = 0; e < EPV; ++e) {
       mx = fmaxf(mx, x[e]);
       mn = x[e] > -INFINITY ? fminf(mn, x[e]) : mn;
+    }
+  };
+  constexpr int U = 4;        // vectors in flight at once
+  for (int32_t i0 = p.v0; i0 < p.v1;) {
+    const int32_t i = i0 + lane;
+    if (row.inside(i0) && row.inside(i0 + (U - 1) * kWave) && i0 + U * kWave <= p.v1) {
+      const u32x4* src = reinterpret_cast<const u32x4*>(row.row + (int64_t)(i * EPV - row.off) * T::kBytes);
+      u32x4 v[U];
+#pragma unroll
+      for (int q = 0; q < U; ++q) v[q] = src[q * kWave];
+#pragma unroll
+      for (int q = 0; q < U; ++q) take(i + q * kWave, v[q], true);
+      i0 += U * kWave;
+    } else {
+      if (i < p.v1) take(i, row.fetch(i), row.inside(i0));
+      i0 += kWave;
     }
   }
   const float own = mx;       // this thread's largest
