@@ -151,7 +151,7 @@ struct SampleShared {
   uint64_t scan[2][kSampleWaves];
   uint64_t part[kSampleWaves], quarter[kSampleQuarters];
   float fmax[kSampleWaves], fmin[kSampleWaves];
-  uint32_t kmin, kmax, n_list;
+  uint32_t kmin, kmax, n_list, n_own;
   int32_t found, bin_whole;   // bin_whole: the cut's bin, if its tokens were one list; else -1
   uint64_t before, weight_before;
   uint64_t cut;                  // the last kept token
@@ -165,6 +165,7 @@ struct Sampler {
   SampleRow<T> row;
   int32_t per, v0, v1;        // vectors of a wave's part; this wave's
   float mx, mn;               // the largest value and the smallest that is finite
+  float own;                  // the largest that this thread has read
   bool infinite;              // the largest was infinite: see get
   float per_bin;
   double scale, top, least, floor_w;   // floor_w: min_p as a weight
@@ -251,13 +252,23 @@ struct Sampler {
       f(i0 + lane, x);
     }
   }
+  // The same for vector i, by itself.
+  __device__ __forceinline__ void get_one(int32_t i, float (&x)[EPV]) const {
+    row.widen(i, i < row.n_lds ? row.lds[i] : row.fetch(i), false, x);
+    if (infinite) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) x[e] = x[e] == INFINITY ? 1.f : __uint_as_float(0x7FC00000u);
+    }
+  }
   // Tokens of lo <= x <= hi for which pick(i, e, x) into the list; n_list counts
-  // also those past its end.
+  // also those past its end.  Where only `few` threads may have seen such a value, the
+  // vectors of those that have are dealt to all (with half of them or more the row is
+  // passed over as it lies).
   template <typename F>
-  __device__ __forceinline__ void collect(float lo, float hi, F&& pick) {
-    if (tid == 0) s.n_list = 0;
+  __device__ __forceinline__ void collect(float lo, float hi, bool few, F&& pick) {
+    if (tid == 0) s.n_list = s.n_own = 0;
     __syncthreads();
-    each([&](int32_t i, const float (&x)[EPV]) {
+    auto take = [&](int32_t i, const float (&x)[EPV]) {
       uint32_t some = 0;
 #pragma unroll
       for (int e = 0; e < EPV; ++e) some |= x[e] >= lo && x[e] <= hi ? 1u << e : 0u;
@@ -271,7 +282,26 @@ struct Sampler {
         const uint32_t at = atomicAdd(&s.n_list, 1u);
         if (at < kSampleList) s.list[at] = (uint64_t)float_key(f) << 32 | (uint32_t)~row.index(i, e);
       }
-    });
+    };
+    uint32_t n = kSampleThreads;
+    if (few) {
+      if (own >= lo) s.lw[atomicAdd(&s.n_own, 1u)] = (uint64_t)tid;
+      __syncthreads();
+      n = s.n_own;
+    }
+    if (n <= kSampleThreads / 2) {
+      const uint32_t steps = (uint32_t)(per + kWave - 1) / kWave;
+      for (uint32_t j = tid; j < n * steps; j += kSampleThreads) {
+        const int32_t step = (int32_t)(j / n), t = (int32_t)s.lw[j - (uint32_t)step * n];
+        const int32_t part = t / kWave * per, i = part + step * kWave + t % kWave;
+        if (i >= min(part + per, row.n_vec)) continue;
+        float x[EPV];
+        get_one(i, x);
+        take(i, x);
+      }
+    } else {
+      each(take);
+    }
     __syncthreads();
   }
   // Values beside which no token of bins b0 .. b1 lies: bin_of's roundings are off by
@@ -388,7 +418,7 @@ struct Sampler {
     __syncthreads();
     const int bin = s.found;
     uint64_t before = s.before, weight_before = s.weight_before;
-    collect(bin_low(bin), bin_high(bin), [&](int32_t, int, float x) { return x >= mn && bin_of(x) == bin; });
+    collect(bin_low(bin), bin_high(bin), false, [&](int32_t, int, float x) { return x >= mn && bin_of(x) == bin; });
     uint32_t n = s.n_list, lo = 0, hi = 0;
     if (tid == 0) s.bin_whole = n <= kSampleList ? bin : -1;
     if (n > kSampleList) {
@@ -451,7 +481,7 @@ struct Sampler {
         __syncthreads();
       }
       if (n <= kSampleList)
-        collect(key_float(lo), key_float(hi), [&](int32_t, int, float) { return true; });
+        collect(key_float(lo), key_float(hi), false, [&](int32_t, int, float) { return true; });
     }
     if (n <= kSampleList) {
       Place p[2];
@@ -585,15 +615,18 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
 
   // The row into LDS; its largest value and the smallest that is finite.
   float mx = -INFINITY, mn = INFINITY;
+  int32_t own_i = 0;          // the first vector in which this thread saw its largest
   auto take = [&](int32_t i, const u32x4& v, bool all) {
     if (i < row.n_lds) row.lds[i] = v;
     float x[EPV];
     row.widen(i, v, all, x);
+    const float before = mx;
 #pragma unroll
     for (int e = 0; e < EPV; ++e) {
       mx = fmaxf(mx, x[e]);
       mn = x[e] > -INFINITY ? fminf(mn, x[e]) : mn;
     }
+    own_i = mx > before ? i : own_i;
   };
   constexpr int U = 4;        // vectors in flight at once
   for (int32_t i0 = p.v0; i0 < p.v1;) {
@@ -611,7 +644,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
       i0 += kWave;
     }
   }
-  const float own = mx;       // this thread's largest
+  p.own = mx;
   if (tid < 128) s.table[tid] = ldexp(exp2((double)tid / 128.0), a.shift);
 #pragma unroll
   for (int m = 1; m < kWave; m <<= 1) {
@@ -642,16 +675,19 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
   p.infinite = mx == INFINITY;             // beside an infinity nothing finite has weight
   if (p.infinite) mx = mn = 1.f;
   if (!(temperature > 0.f) || top_k == 1 || min_p > 1.f) {     // the first of the largest
-    p.each([&](int32_t i, const float (&x)[EPV]) {
-      uint32_t first = 0xFFFFFFFFu;
+    if (p.own == (p.infinite ? INFINITY : mx)) {
+      float x[EPV];
+      row.widen(own_i, own_i < row.n_lds ? row.lds[own_i] : row.fetch(own_i), false, x);
+      uint32_t first = 0;
 #pragma unroll
-      for (int e = EPV - 1; e >= 0; --e) first = x[e] == mx ? row.index(i, e) : first;
-      if (first != 0xFFFFFFFFu) atomicMin(&s.index, first);
-    });
+      for (int e = EPV - 1; e >= 0; --e) first = x[e] == p.own ? row.index(own_i, e) : first;
+      atomicMin(&s.index, first);
+    }
     __syncthreads();
     if (tid == 0) a.tokens[r] = (int32_t)s.index;
     return;
   }
+  if (p.infinite) p.own = p.own == INFINITY ? 1.f : -INFINITY;
   p.mx = mx;
   p.mn = mn;
   p.top = (double)mx;
@@ -671,8 +707,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
     // A bin up to which at least top_k tokens lie: that of the k-th largest of the
     // threads' own largest values, or, for a larger k, of the k-th largest of all.
     if (top_k <= kSampleTopK) {
-      const float first = p.infinite ? (own == INFINITY ? 1.f : -INFINITY) : own;
-      if (p.valid(first)) atomicAdd(&s.count[p.bin_of(first)], 1u);
+      if (p.valid(p.own)) atomicAdd(&s.count[p.bin_of(p.own)], 1u);
     } else {
       p.each([&](int32_t, const float (&x)[EPV]) {
 #pragma unroll
@@ -688,7 +723,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
     __syncthreads();
     const int bin = s.found;       // (fewer than k counted: every bin)
     s.count[tid] = 0;
-    p.collect(fmaxf(p.bin_low(bin), mn), mx, [&](int32_t, int, float x) { return p.bin_of(x) <= bin; });
+    p.collect(fmaxf(p.bin_low(bin), mn), mx, top_k <= kSampleTopK, [&](int32_t, int, float x) { return p.bin_of(x) <= bin; });
     const uint32_t n = s.n_list;
     if (n <= kSampleList) {
       typename Sampler<T>::Place q[2];
@@ -801,7 +836,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
       // a value below which min_p keeps nothing: T ln(min_p) under the maximum, and some more
       const float depth = -1.01f * temperature * logf(fmaxf(min_p, 1e-37f)) + 1e-5f * fabsf(mx) + 1e-30f;
       const float low = want_m && mx - depth > cut_x ? mx - depth : cut_x;
-      p.collect(low, mx, [&](int32_t i, int e, float x) { return kept(i, e, x) != 0; });
+      p.collect(low, mx, want_m, [&](int32_t i, int e, float x) { return kept(i, e, x) != 0; });
       const uint32_t n = s.n_list;
       if (n <= kSampleList) {
         uint64_t id[2], g[2];

@@ -155,6 +155,39 @@ def test_rows_apart_and_at_odd_addresses():
             check(wide[:, first:first + 1000], rng.random(13).tolist(), **draw_params(rng, 13))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [20000, 131073])
+def test_largest_values_in_few_places(dtype, vocab):
+    """The tokens that can be drawn lie side by side, at either end, or anywhere, also
+    with equal ones and infinities among them; greedy rows take the first of equals."""
+    rng = np.random.default_rng(vocab)
+    l = rng.standard_normal((12, vocab)).astype(np.float32)
+    l[1, 9000:9700] += 8.0
+    l[2, :700] += 8.0
+    l[3, -700:] += 8.0
+    l[4, 11::64] += 8.0                                   # a few per lane, everywhere
+    l[5, [vocab - 1, 12345, 12344, 77]] = 30.0            # equal ones
+    l[6, [vocab - 2, 19000, 18999]] = np.inf
+    l[7, 5000:5040] = np.inf
+    l[8] = -np.inf
+    l[8, vocab - 3] = -1e30
+    l[9, ::2] = np.nan
+    l[10, 100:] = -np.inf
+    l[11, 600:] = l[11, 0]
+    wide = torch.full((12, vocab + 3), 99.0, dtype=DT[dtype], device="cuda")
+    wide[:, 1:vocab + 1] = torch.from_numpy(l).cuda().to(DT[dtype])
+    logits = wide[:, 1:vocab + 1]
+    u = rng.random(12).tolist()
+    check(logits, u, temperature=[0.0] * 12)
+    check(logits, u, min_p=[1.5] * 12)
+    for k in (1, 2, 50, 511, 512, 513, 1536, 1537):
+        check(logits, u, top_k=[k] * 12)
+    check(logits, u, top_k=[400] * 12, top_p=[0.9] * 12, min_p=[0.02] * 12)
+    for m in (0.9, 0.05, 1e-3):
+        check(logits, u, min_p=[m] * 12)
+        check(logits, u, min_p=[m] * 12, top_p=[0.8] * 12)
+
+
 def test_frequencies():
     """Tokens come as often as their weights say: u over a grid of 4096 places hits
     each token within one place of its share, for any rounding of the sums."""
