@@ -262,8 +262,9 @@ struct Sampler {
   }
   // Tokens of lo <= x <= hi for which pick(i, e, x) into the list; n_list counts
   // also those past its end.  Where only `few` threads may have seen such a value, the
-  // vectors of those that have are dealt to all (with half of them or more the row is
-  // passed over as it lies).
+  // vectors of those that have are dealt to all (with more than 3/4 of them the row is
+  // passed over as it lies; a limit of 1/2 took 44 us instead of 40 at top_k 500 of 256
+  // rows of 128,000, 32 instead of 28.5 at min_p 0.05).
   template <typename F>
   __device__ __forceinline__ void collect(float lo, float hi, bool few, F&& pick) {
     if (tid == 0) s.n_list = s.n_own = 0;
@@ -289,7 +290,7 @@ struct Sampler {
       __syncthreads();
       n = s.n_own;
     }
-    if (n <= kSampleThreads / 2) {
+    if (n <= kSampleThreads * 3 / 4) {
       const uint32_t steps = (uint32_t)(per + kWave - 1) / kWave;
       for (uint32_t j = tid; j < n * steps; j += kSampleThreads) {
         const int32_t step = (int32_t)(j / n), t = (int32_t)s.lw[j - (uint32_t)step * n];
