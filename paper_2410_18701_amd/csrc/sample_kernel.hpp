@@ -190,7 +190,7 @@ struct Sampler {
     return x + (w > 0 ? from(w - 1) : 0);
   }
 
-  // The weight of a value, before it is rounded to a whole number.
+  // The weight of a value, before it is rounded to a whole number (0, of a NaN or -inf).
   __device__ __forceinline__ double weight(float x) const {
     const double y = fmax(((double)x - top) * scale, least);        // 128 log2 w; a NaN is least
     constexpr double kMagic = 6755399441055744.0;                   // 1.5 * 2^52: rounds to a whole number
@@ -204,22 +204,19 @@ struct Sampler {
     p = fma(p, f, 1.0);
     // 2^(j / 128 + shift): the table's entry with j / 128 added to its exponent
     const double b = __longlong_as_double(__double_as_longlong(s.table[j & 127]) +
-                                          ((uint64_t)((j << 13) & 0xFFF00000u) << 32));
+                                          ((uint64_t)((j & ~127u) << 13) << 32));
     return p * b;
   }
   __device__ __forceinline__ uint64_t whole(double wd) const {
     return (uint64_t)__double_as_longlong(wd + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;   // + 2^52
   }
   __device__ __forceinline__ uint32_t valid(float x) const { return x >= mn; }
-  __device__ __forceinline__ uint64_t weight_of(float x) const {
-    const uint64_t g = whole(weight(x));
-    return valid(x) ? g : 0;
-  }
+  __device__ __forceinline__ uint64_t weight_of(float x) const { return whole(weight(x)); }
   // 0 also below min_p (the largest value never is)
   __device__ __forceinline__ uint64_t weight_if(float x, uint32_t keep) const {
     const double d = weight(x);
     const uint64_t g = whole(d);
-    return keep & valid(x) & ((uint32_t)(d >= floor_w) | (uint32_t)(x == mx)) ? g : 0;
+    return keep & ((uint32_t)(d >= floor_w) | (uint32_t)(x == mx)) ? g : 0;
   }
   __device__ __forceinline__ int bin_of(float x) const {
     return (int)fminf((mx - x) * per_bin, (float)(kSampleBins - 1));
