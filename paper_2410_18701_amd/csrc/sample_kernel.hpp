@@ -339,7 +339,14 @@ struct Sampler {
               s.list[h] = x;
             }
           }
-          __syncthreads();
+          // A wave's 64 pairs at distances up to 64 are 128 elements of its own, which its
+          // own operations on LDS, done in order, pass on; only others are waited for.
+          if (j > kWave || (j == 1 && k > kWave)) {
+            __syncthreads();
+          } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+          }
         }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
