@@ -509,7 +509,8 @@ baton_status baton_silu_mul(int32_t dtype, const void* gate_up, void* out, int32
  * accumulate = 1 adding to y (what baton_linear_packed left there), 0
  * overwriting it.  row_adapter: host array of rows entries, each an index into
  * adapters (host array of n_adapters; only those named by a row are read) or
- * -1 for none: such a row is zeros (accumulate = 0) or left as it is (1).
+ * -1 for none: such a row is zeros (accumulate = 0) or left as it is (1).  Both
+ * arrays are read during the call, so a captured call keeps what they held.
  * Projections fused along their outputs (query, key and value; gate and up)
  * have an adapter for each part: the output's columns are n_parts ranges of
  * part_dims[p] (host array; NULL with one part: all of out_dim), A_i holds

@@ -53,6 +53,8 @@ class Adapters:
             for t in (ai, bi):
                 if t.dtype != torch.bfloat16 or not t.is_contiguous():
                     raise ValueError("Adapters: contiguous bf16 tensors only")
+                if t.device != self.a[0].device:
+                    raise ValueError("Adapters: tensors on different devices")
             self.table[i] = B.baton_adapter(ai.data_ptr(), bi.data_ptr(), bi.shape[1], float(s))
         self.in_dim = self.a[0].shape[1] if self.n else None
         self.out_dim = self.b[0].shape[0] if self.n else None
@@ -210,7 +212,7 @@ class DecodeLayers:
     adapters[layer]: dict from names of PROJ to Adapters (qkv in parts [Hq D, Hkv D,
     Hkv D], gate_up in [F, F], the same adapter at the same index everywhere);
     slot_adapter[slot] is the index its query uses, -1 for none, and may be changed
-    between steps.  head: dict of norm [hid] and out [vocab][hid], for next_tokens."""
+    between steps (a captured step keeps the indices that it was captured with).  head: dict of norm [hid] and out [vocab][hid], for next_tokens."""
 
     PROJ = ("qkv", "o", "gate_up", "down")
 

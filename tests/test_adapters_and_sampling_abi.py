@@ -64,7 +64,9 @@ def test_adapters_wrapper_refusals():
                 lambda: Adapters([t(16, 64, d=torch.float32)], [t(32, 16)], [1.0]),
                 lambda: Adapters([t(64, 16).t()], [t(32, 16)], [1.0]),
                 lambda: Adapters([t(32, 64)], [t(32, 16)], [1.0], parts=[8, 8]),
-                lambda: Adapters([t(8, 64), t(8, 72)], [t(32, 8), t(32, 8)], [1.0, 1.0])):
+                lambda: Adapters([t(8, 64), t(8, 72)], [t(32, 8), t(32, 8)], [1.0, 1.0]),
+                lambda: Adapters([t(16, 64)], [t(32, 16).to("meta")], [1.0]),
+                lambda: Adapters([t(8, 64), t(8, 64).to("meta")], [t(32, 8), t(32, 8)], [1.0, 1.0])):
         with pytest.raises(ValueError):
             bad()
 
