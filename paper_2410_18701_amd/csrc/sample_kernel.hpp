@@ -257,8 +257,8 @@ struct Sampler {
       for (int e = 0; e < EPV; ++e) x[e] = x[e] == INFINITY ? 1.f : __uint_as_float(0x7FC00000u);
     }
   }
-  // Tokens of lo <= x <= hi for which pick(i, e, x) into the list; n_list counts
-  // also those past its end.  Where only `few` threads may have seen such a value, the
+  // Tokens of lo <= x <= hi for which pick(i, e, x) into the list; n_list is more than it
+  // holds if they are, which ends the search.  Where only `few` threads may have seen such a value, the
   // vectors of those that have are dealt to all (with more than 3/4 of them the row is
   // passed over as it lies; a limit of 1/2 took 44 us instead of 40 at top_k 500 of 256
   // rows of 128,000, 32 instead of 28.5 at min_p 0.05).
@@ -266,10 +266,12 @@ struct Sampler {
   __device__ __forceinline__ void collect(float lo, float hi, bool few, F&& pick) {
     if (tid == 0) s.n_list = s.n_own = 0;
     __syncthreads();
+    uint32_t last = 0;     // this thread's latest place
     auto take = [&](int32_t i, const float (&x)[EPV]) {
       uint32_t some = 0;
 #pragma unroll
       for (int e = 0; e < EPV; ++e) some |= x[e] >= lo && x[e] <= hi ? 1u << e : 0u;
+      if (last >= kSampleList) some = 0;
       while (some) {
         const int e = __builtin_ctz(some);
         some &= some - 1;
@@ -279,6 +281,7 @@ struct Sampler {
         if (!pick(i, e, f)) continue;
         const uint32_t at = atomicAdd(&s.n_list, 1u);
         if (at < kSampleList) s.list[at] = (uint64_t)float_key(f) << 32 | (uint32_t)~row.index(i, e);
+        last = at;
       }
     };
     uint32_t n = kSampleThreads;
