@@ -21,7 +21,7 @@
 // and the latency of its dependent steps, so whole passes over the row are kept few
 // and a list of tokens in LDS takes their place as soon as one can:
 //  * top_k up to 512: the k-th largest of the threads' own largest values bounds
-//    the k-th largest from below (up to 1536, counts in bins of the values do); the
+//    the k-th largest from below (up to 1024, counts in bins of the values do); the
 //    tokens from there on, a few more than k, are the list.
 //  * else 1024 bins of equal width over the top of the values' range hold counts
 //    or weights (floats' own bits would put most tokens into a few bins, whose atomics
@@ -33,9 +33,9 @@
 //    weights per wave, then the tokens of the wave's part in which the target lies.
 // exp: 2^(j / 128) from a table, times a polynomial of degree 4 on half a step:
 // relative error below 2^-49.
-// us, bf16: one row of 32,000 8 (greedy), 13 (top_k 50), 15 (temperature alone), 23 to
-// 26 (top_p); 256 rows of 128,000, which LDS holds a third of, 25, 32, 49 and 80 to 88,
-// of which 13.5 is the first read and 36 the bins' weights.
+// us, bf16: one row of 32,000 8 (greedy), 12 (top_k 50), 15 (temperature alone), 23 to
+// 26 (top_p); 256 rows of 128,000, which LDS holds a third of, 15, 21, 46 and 72 to 85,
+// of which 13.5 is the first read and 33 the bins' weights.
 #pragma once
 
 #include "common.hpp"
@@ -48,7 +48,7 @@ constexpr int kSampleBins = 1024;        // == kSampleThreads: a bin per thread
 constexpr int kSampleList = 2048;        // tokens in a list at most, two per thread
 constexpr int kSampleRank = 256;         // up to here a list is ordered by counting, not sorted
 constexpr int kSampleTopK = 512;         // the largest top_k for which threads' largest values bound it
-constexpr int kSampleTopKList = 1536;    // and the largest whose tokens are gathered as a list
+constexpr int kSampleTopKList = kSampleThreads;   // and the largest whose tokens are gathered as a list
 constexpr int kSampleQuarters = 4;       // of the row, with bins of their own
 constexpr int kSampleRowBytes = 80 << 10;    // of a row kept in LDS
 
@@ -220,6 +220,14 @@ struct Sampler {
   }
   __device__ __forceinline__ int bin_of(float x) const {
     return (int)fminf((mx - x) * per_bin, (float)(kSampleBins - 1));
+  }
+
+  // Counts the token in its bin; those of the last one, which may be most of the row, in `deep`.
+  __device__ __forceinline__ void count(float x, uint32_t& deep) {
+    if (!valid(x)) return;
+    const int b = bin_of(x);
+    if (b == kSampleBins - 1) ++deep;
+    else atomicAdd(&s.count[b], 1u);
   }
 
   // The elements of vector i0 + lane (i0 the same in the wave), NaN outside the row
@@ -714,13 +722,23 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
   if (want_k && top_k <= kSampleTopKList) {
     // A bin up to which at least top_k tokens lie: that of the k-th largest of the
     // threads' own largest values, or, for a larger k, of the k-th largest of all.
+    // The bins span the threads' largest values, whatever the temperature.
+    float low = p.own > -INFINITY ? p.own : mx;
+#pragma unroll
+    for (int m = 1; m < kWave; m <<= 1) low = fminf(low, __shfl_xor(low, m, kWave));
+    if (lane == 0) s.part[w] = __float_as_uint(low);
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < kSampleWaves; ++v) low = fminf(low, __uint_as_float((uint32_t)s.part[v]));
+    const float weight_bins = p.per_bin;
+    if (mx > low) p.per_bin = fminf((float)(kSampleBins - 2) / (mx - low), 3.4e38f);
     if (top_k <= kSampleTopK) {
       if (p.valid(p.own)) atomicAdd(&s.count[p.bin_of(p.own)], 1u);
     } else {
       p.each([&](int32_t, const float (&x)[EPV]) {
 #pragma unroll
         for (int e = 0; e < EPV; ++e)
-          if (p.valid(x[e])) atomicAdd(&s.count[p.bin_of(x[e])], 1u);
+          if (x[e] >= low) atomicAdd(&s.count[p.bin_of(x[e])], 1u);
       });
     }
     __syncthreads();
@@ -756,9 +774,11 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
       p.draw_list(n, u, id, g, at, a.tokens + r);
       return;
     }
+    p.per_bin = weight_bins;
   }
   if (want_k || want_p) {
     uint64_t* const weights = s.weight[w / (kSampleWaves / kSampleQuarters)];
+    uint32_t deep = 0;
     p.each([&](int32_t, const float (&x)[EPV]) {
 #pragma unroll
       for (int h = 0; h < EPV; h += 4) {
@@ -773,11 +793,11 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
         }
         if (want_k) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (p.valid(x[h + e])) atomicAdd(&s.count[p.bin_of(x[h + e])], 1u);
+          for (int e = 0; e < 4; ++e) p.count(x[h + e], deep);
         }
       }
     });
+    if (deep) atomicAdd(&s.count[kSampleBins - 1], deep);
     __syncthreads();
     const uint64_t bin_count = s.count[tid];
     uint64_t bin_weight = 0;

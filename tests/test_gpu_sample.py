@@ -180,8 +180,9 @@ def test_largest_values_in_few_places(dtype, vocab):
     u = rng.random(12).tolist()
     check(logits, u, temperature=[0.0] * 12)
     check(logits, u, min_p=[1.5] * 12)
-    for k in (1, 2, 50, 511, 512, 513, 1536, 1537):
+    for k in (1, 2, 50, 511, 512, 513, 1024, 1025, 1536, 1537):
         check(logits, u, top_k=[k] * 12)
+        check(logits, u, top_k=[k] * 12, temperature=[0.02, 0.1, 0.5] * 4)
     check(logits, u, top_k=[400] * 12, top_p=[0.9] * 12, min_p=[0.02] * 12)
     for m in (0.9, 0.05, 1e-3):
         check(logits, u, min_p=[m] * 12)
