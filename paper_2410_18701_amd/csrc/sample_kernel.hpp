@@ -145,7 +145,7 @@ struct SampleShared {
   uint64_t weight[kSampleQuarters][kSampleBins];
   uint32_t count[kSampleBins];
   uint64_t list[kSampleList];    // tokens: (float_key, ~index), so that larger is earlier
-  uint64_t lw[kSampleList];      // their weights
+  uint64_t lw[kSampleList];      // their weights; before they are known, scratch
   uint64_t ahead_w[kSampleRank];
   uint32_t ahead[kSampleRank];
   uint64_t scan[2][kSampleWaves];
@@ -439,6 +439,9 @@ struct Sampler {
     if (tid == 0) s.bin_whole = n <= kSampleList ? bin : -1;
     if (n > kSampleList) {
       // Too many: bins over the keys of [lo, hi] until the list holds them or one key is left.
+      // Their weights lie in lw, free until the list is ordered: s.weight keeps the bins of
+      // the whole row, which the draw reads once the other prefix has ended.
+      static_assert(kSampleBins <= kSampleList, "weights of the narrower bins");
       if (tid == 0) {
         s.kmin = 0xFFFFFFFFu;
         s.kmax = 0;
@@ -462,7 +465,7 @@ struct Sampler {
       hi = s.kmax;
       while (n > kSampleList && lo < hi) {
         const int sh = max(0, 22 - __clz((int)(hi - lo)));     // (hi - lo) >> sh < 1024
-        s.weight[0][tid] = 0;
+        s.lw[tid] = 0;
         s.count[tid] = 0;
         __syncthreads();
         each([&](int32_t, const float (&x)[EPV]) {
@@ -471,13 +474,13 @@ struct Sampler {
             const uint32_t k = float_key(x[e]);
             if (valid(x[e]) && k >= lo && k <= hi) {
               atomicAdd(&s.count[(hi - k) >> sh], 1u);
-              atomicAdd(reinterpret_cast<unsigned long long*>(&s.weight[0][(hi - k) >> sh]),
+              atomicAdd(reinterpret_cast<unsigned long long*>(&s.lw[(hi - k) >> sh]),
                         (unsigned long long)weight_of(x[e]));
             }
           }
         });
         __syncthreads();
-        const uint64_t c = s.count[tid], g = s.weight[0][tid];
+        const uint64_t c = s.count[tid], g = s.lw[tid];
         uint64_t total;
         const uint64_t tc = wg_scan(c, total), tg = wg_scan(g, total);
         const uint64_t m = by_weight ? g : c, t = before + (by_weight ? tg : tc);

@@ -83,6 +83,22 @@ def test_crowded_bins(dtype):
           top_k=rng.choice([0, 3, 2500, 20000], rows).tolist(), top_p=rng.choice([0.1, 0.5, 0.99, 1.0], rows).tolist())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [5000, 32000, 128000])
+def test_a_nucleus_above_a_crowded_cut_by_count(dtype, vocab):
+    """top_k past what a list holds ends among thousands of different values of one
+    bin (most of the row lies more than 32 temperatures below the maximum), top_p in
+    a bin of few: each prefix by its own sums, wherever in the row the weight is."""
+    rng = np.random.default_rng(vocab + len(dtype))
+    combos = [(t, k, p) for t in (0.1, 0.3) for k in (2000, vocab // 3, vocab - 1) for p in (0.5, 0.9, 0.99)]
+    us = (np.arange(8) + rng.random()) / 8
+    t, k, p, u = (list(x) for x in zip(*[c + (float(x),) for c in combos for x in us]))
+    l = rng.standard_normal((len(u), vocab)).astype(np.float32) * 4
+    l[::3, :vocab // 4] += 3.0            # the weight in the first quarter of the row, ...
+    l[1::3, vocab * 3 // 4:] += 3.0       # ... in the last, anywhere
+    check(torch.from_numpy(l).cuda().to(DT[dtype]), u, temperature=t, top_k=k, top_p=p)
+
+
 def test_many_neighbours_of_a_large_vocabulary():
     """More kept tokens side by side than one range of the list's draw takes."""
     vocab, n = 1 << 21, 1500
