@@ -10,11 +10,11 @@
 //    the launch has a few waves per SIMD whatever the number of adapters; each
 //    range's sums go to the workspace in fp32.
 //  * up: the ranges' sums are added in order, scaled, and split into two bf16
-//    halves (the value and what its rounding leaves: 16 bits of it), staged in LDS;
+//    halves (its first bits and what they leave: 16 bits of it), staged in LDS;
 //    then 16 x 16 tiles of y = h . B^T, every wave its own columns, the next 32
 //    columns of B and of y's first rows on their way meanwhile.  The second half
 //    costs one more matrix operation on operands that are in registers; without it
-//    h would be rounded to 8 bits.
+//    h would be cut to 8 bits.
 // Sums are fp32 in a fixed order: the same call gives the same bits.
 // us down / up: 64 rows of 24 adapters of rank 32, 4096 to 3 parts of 4096 (35 MB)
 // 7.0 / 8.2; 240 rows of 40 of rank 64, 4096 to 2 of 11008 (177 MB with y) 15.4 / 32.7.
@@ -59,10 +59,14 @@ struct AdapterArgs {
 };
 static_assert(sizeof(AdapterArgs) <= 4096, "kernel arguments");
 
-// f as two bf16 halves; nothing remains of what rounds to an infinity (or is one, or a NaN).
+// f as two bf16 halves that sum to it within 2^-16 of it.  The first is cut off, not
+// rounded, and the last bit of f set, so that the second has f's sign and is not 0 where f
+// is not: times an infinity of B both are the same infinity, and times 0 both are 0.
+// An infinity or a NaN (a product's, so a quiet one) is both halves.
 __device__ __forceinline__ void adapter_split(float f, uint32_t& hi, uint32_t& lo) {
-  hi = f32_to_bf16_rne(f);
-  lo = (hi & 0x7F80u) == 0x7F80u ? 0u : f32_to_bf16_rne(f - __uint_as_float(hi << 16));
+  const uint32_t b = __float_as_uint(f);
+  hi = b >> 16;
+  lo = (hi & 0x7F80u) == 0x7F80u ? hi : f32_to_bf16_rne(__uint_as_float(b | 1u) - __uint_as_float(hi << 16));
 }
 
 __device__ __forceinline__ ad_bf16x8 ad_vec(const u32x4& w) { return __builtin_bit_cast(ad_bf16x8, w); }

@@ -123,6 +123,32 @@ def test_rows_do_not_mix_and_infinities_stay():
     assert (wide[21:] == 7.0).all()
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("rows,in_dim,part_dims,rank", [(3, 128, [48], 8), (20, 256, [40, 24], 24), (5, 136, [64], 40),
+                                                        (70, 64, [32], 104)])
+def test_infinities_of_b(rows, in_dim, part_dims, rank, accumulate):
+    """An infinite element of B times a number other than 0 is an infinity of its sign, in its
+    column alone; infinities of both signs, and an infinity times 0, are NaN."""
+    rng = np.random.default_rng(rank)
+    x, a, b, scales, y0 = make(rng, rows, in_dim, part_dims, [rank])
+    inf = float("inf")
+    b[0][1, 0], b[0][7, rank - 1], b[0][9, 3] = inf, -inf, inf
+    b[0][12, 2], b[0][12, 5] = inf, -inf        # of one sign where the two products agree
+    x[rows - 1] = 0.0
+    scales[0] = -1.5
+    y = y0.clone()
+    Gemm().linear_adapters(x, Adapters(a, b, scales, parts=part_dims), [0] * rows, y, accumulate=accumulate)
+    with np.errstate(invalid="ignore"):
+        h, mag = val(x)[:-1] @ val(a[0]).T, np.abs(val(x)[:-1]) @ np.abs(val(a[0])).T
+        assert (np.abs(h) > in_dim * 2.0 ** -24 * mag).all()   # fp32 sums have its sign
+        o, tol = want(x, a, b, scales, [0] * rows, part_dims, y0, accumulate)
+        got, finite = val(y), np.isfinite(o)
+        assert np.array_equal(np.isnan(got), np.isnan(o))
+        assert np.array_equal(got[np.isinf(o)], o[np.isinf(o)])
+        assert (np.abs(got - o)[finite] <= tol[finite]).all()
+    assert np.isinf(o).any() and np.isnan(o[:-1]).any() and np.isnan(o[-1]).sum() == 4
+
+
 def test_beside_a_packed_projection_in_a_hip_graph():
     """The projection and its adapters captured and replayed, other work between the replays."""
     rng = np.random.default_rng(8)
