@@ -519,9 +519,9 @@ baton_status baton_silu_mul(int32_t dtype, const void* gate_up, void* out, int32
  * x: device [rows <= BATON_GEMM_MAX_ROWS][in_dim], y: device [rows][out_dim];
  * bf16, 16-byte aligned, y apart from everything read.  Ranks may differ
  * between adapters (multiples of 8 up to BATON_ADAPTER_MAX_RANK; a smaller one
- * is padded with zero rows of A and columns of B).  Products and sums are in
- * fp32 (x . A^T is kept to 16 bits), in a fixed order, and y is rounded once;
- * infinities and NaN come out as those products and sums give them.
+ * is padded with zero rows of A and columns of B).  Products and sums, x . A^T
+ * among them, are in fp32 in a fixed order, and y is rounded once; infinities and
+ * NaN come out as those products and sums give them.
  * ws: device workspace of at least baton_linear_adapters_workspace_bytes(rows,
  * n_parts, the largest rank a row uses), 16-byte aligned; a multiple of that
  * lets in_dim be divided over more workgroups.  Calls that share a workspace go

@@ -9,12 +9,13 @@
 //    waves divide the range and add through LDS.  Ranges are taken so that
 //    the launch has a few waves per SIMD whatever the number of adapters; each
 //    range's sums go to the workspace in fp32.
-//  * up: the ranges' sums are added in order, scaled, and split into two bf16
-//    halves (its first bits and what they leave: 16 bits of it), staged in LDS;
-//    then 16 x 16 tiles of y = h . B^T, every wave its own columns, the next 32
-//    columns of B and of y's first rows on their way meanwhile.  The second half
-//    costs one more matrix operation on operands that are in registers; without it
-//    h would be cut to 8 bits.
+//  * up: the ranges' sums are added in order, scaled, and split into three bf16
+//    parts, which keep all 24 bits, staged in LDS; then 16 x 16 tiles of
+//    y = h . B^T, every wave its own columns, the next 32 columns of B and of y's
+//    first rows on their way meanwhile.  The second and third part cost a matrix
+//    operation each on operands of B that are in registers (up to 0.1 us of the times
+//    below); with one part h would be rounded to 8 bits, with two to 16, which still
+//    turns one rounding of y in some 250 the other way.
 // Sums are fp32 in a fixed order: the same call gives the same bits.
 // us down / up: 64 rows of 24 adapters of rank 32, 4096 to 3 parts of 4096 (35 MB)
 // 7.0 / 8.2; 240 rows of 40 of rank 64, 4096 to 2 of 11008 (177 MB with y) 15.4 / 32.7.
@@ -35,6 +36,7 @@ constexpr int kAdapterRows = 64;      // batch rows a workgroup takes at most
 constexpr int kAdapterMaxRank = 128;  // == BATON_ADAPTER_MAX_RANK
 constexpr int kAdapterGroups = 96;    // adapters per launch (the arguments are 4 KB at most)
 constexpr int kAdapterMaxRows = 256;  // == BATON_GEMM_MAX_ROWS
+constexpr int kAdapterParts = 3;      // bf16 parts of x . A^T
 
 // The rows of one adapter: places [begin, next group's begin) of the sorted rows.
 struct AdapterGroup {
@@ -59,14 +61,29 @@ struct AdapterArgs {
 };
 static_assert(sizeof(AdapterArgs) <= 4096, "kernel arguments");
 
-// f as two bf16 halves that sum to it within 2^-16 of it.  The first is cut off, not
-// rounded, and the last bit of f set, so that the second has f's sign and is not 0 where f
-// is not: times an infinity of B both are the same infinity, and times 0 both are 0.
-// An infinity or a NaN (a product's, so a quiet one) is both halves.
-__device__ __forceinline__ void adapter_split(float f, uint32_t& hi, uint32_t& lo) {
+// f in three bf16 parts that sum to it within 2^-23 of it.  Each is what the one before
+// left, cut off (the last rounded) with its last bit set, so that all have f's sign and
+// none is 0 where f is not: times an infinity of B all are the same infinity, and times 0
+// all are 0 (numbers under 2^-80, whose last part is too small for bf16, lose it).  An
+// infinity or a NaN (a product's, so a quiet one) is every part.
+__device__ __forceinline__ void adapter_split(float f, uint32_t (&part)[kAdapterParts]) {
   const uint32_t b = __float_as_uint(f);
-  hi = b >> 16;
-  lo = (hi & 0x7F80u) == 0x7F80u ? hi : f32_to_bf16_rne(__uint_as_float(b | 1u) - __uint_as_float(hi << 16));
+  part[0] = b >> 16;
+  const uint32_t r = __float_as_uint(__uint_as_float(b | 1u) - __uint_as_float(b & 0xFFFF0000u));
+  part[1] = r >> 16;
+  part[2] = f32_to_bf16_rne(__uint_as_float(r | 1u) - __uint_as_float(r & 0xFFFF0000u));
+  if ((b & 0x7F800000u) == 0x7F800000u) part[1] = part[2] = part[0];
+}
+
+// The parts of four elements v, staged one below the other `plane` elements apart.
+__device__ __forceinline__ void adapter_stage(const ad_f32x4& v, uint16_t* at, int32_t plane) {
+  uint32_t part[4][kAdapterParts];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) adapter_split(v[e], part[e]);
+#pragma unroll
+  for (int q = 0; q < kAdapterParts; ++q)
+    *reinterpret_cast<uint2*>(at + q * plane) =
+        make_uint2(part[0][q] | part[1][q] << 16, part[2][q] | part[3][q] << 16);
 }
 
 __device__ __forceinline__ ad_bf16x8 ad_vec(const u32x4& w) { return __builtin_bit_cast(ad_bf16x8, w); }
@@ -165,13 +182,13 @@ __device__ __forceinline__ void adapter_columns(const AdapterArgs& a, int local,
 template <int NKK>
 constexpr int adapter_row() { return 32 * NKK + 8; }
 
-// Ranks up to 32 * NKK; `lds_rows` rows of h (whole tiles of 16) are staged twice
-// in the launch's dynamic LDS.
+// Ranks up to 32 * NKK; the parts of `lds_rows` rows of h (whole tiles of 16) are
+// staged in the launch's dynamic LDS.
 template <int NKK>
 __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const AdapterArgs a, const int32_t lds_rows) {
   constexpr int ROW = adapter_row<NKK>();
-  extern __shared__ __attribute__((aligned(16))) uint16_t hs_hi[];
-  uint16_t* const hs_lo = hs_hi + lds_rows * ROW;
+  extern __shared__ __attribute__((aligned(16))) uint16_t hs[];
+  const int32_t plane = lds_rows * ROW;
   const int gi = adapter_group<true>(a, blockIdx.x);
   const AdapterGroup& g = a.g[gi];
   const int local = (int)blockIdx.x - (gi > 0 ? a.g[gi - 1].up_end : 0);
@@ -216,11 +233,7 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
 #pragma unroll 4
       for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const ad_f32x4*>(src + (int64_t)s * a.rows * a.hs);
     }
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) adapter_split(v[e] * g.scale, hi[e], lo[e]);
-    *reinterpret_cast<uint2*>(hs_hi + r * ROW + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-    *reinterpret_cast<uint2*>(hs_lo + r * ROW + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+    adapter_stage(v * g.scale, hs + r * ROW + j, plane);
   }
   __syncthreads();
   for (int c = w0; c < w1; c += 32) {
@@ -237,12 +250,11 @@ __global__ void __launch_bounds__(kWave * kAdapterWaves) adapter_up_kernel(const
       ad_f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) {
-        const ad_bf16x8 hi = ad_vec(*reinterpret_cast<const u32x4*>(hs_hi + r * ROW + 32 * kk + 8 * g4));
-        const ad_bf16x8 lo = ad_vec(*reinterpret_cast<const u32x4*>(hs_lo + r * ROW + 32 * kk + 8 * g4));
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j][kk]), lo, acc[j], 0, 0, 0);
-          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j][kk]), hi, acc[j], 0, 0, 0);
+        for (int q = kAdapterParts - 1; q >= 0; --q) {
+          const ad_bf16x8 h = ad_vec(*reinterpret_cast<const u32x4*>(hs + q * plane + r * ROW + 32 * kk + 8 * g4));
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j][kk]), h, acc[j], 0, 0, 0);
         }
       }
       u32x4 o;
@@ -272,7 +284,7 @@ template <int AT>
 __global__ void __launch_bounds__(kWave * kAdapterSmallWaves) adapter_small_kernel(const AdapterArgs a) {
   constexpr int NW = kAdapterSmallWaves, ROW = adapter_row<1>(), U = 8 / AT;   // U steps' loads in flight
   __shared__ ad_f32x4 part[NW][AT][kWave];
-  __shared__ __attribute__((aligned(16))) uint16_t hs_hi[16 * ROW], hs_lo[16 * ROW];
+  __shared__ __attribute__((aligned(16))) uint16_t hs[kAdapterParts][16 * ROW];
   const int gi = adapter_group<true>(a, blockIdx.x);
   const AdapterGroup& g = a.g[gi];
   const int local = (int)blockIdx.x - (gi > 0 ? a.g[gi - 1].up_end : 0);
@@ -331,21 +343,20 @@ __global__ void __launch_bounds__(kWave * kAdapterSmallWaves) adapter_small_kern
       for (int q = 0; q < NW; ++q) v += part[q][w][lane];
     }
     const int j = 16 * w + 4 * g4;
-    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) adapter_split(c16 < n && j < rank ? v[e] * g.scale : 0.f, hi[e], lo[e]);
-    *reinterpret_cast<uint2*>(hs_hi + c16 * ROW + j) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-    *reinterpret_cast<uint2*>(hs_lo + c16 * ROW + j) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+    for (int e = 0; e < 4; ++e) v[e] = c16 < n && j + e < rank ? v[e] * g.scale : 0.f;
+    adapter_stage(v, hs[0] + c16 * ROW + j, 16 * ROW);
   }
   __syncthreads();
-  const ad_bf16x8 hi = ad_vec(*reinterpret_cast<const u32x4*>(hs_hi + c16 * ROW + 8 * g4));
-  const ad_bf16x8 lo = ad_vec(*reinterpret_cast<const u32x4*>(hs_lo + c16 * ROW + 8 * g4));
+  ad_bf16x8 h[kAdapterParts];
+#pragma unroll
+  for (int q = 0; q < kAdapterParts; ++q) h[q] = ad_vec(*reinterpret_cast<const u32x4*>(hs[q] + c16 * ROW + 8 * g4));
   u32x4 o;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     ad_f32x4 d = {0.f, 0.f, 0.f, 0.f};
-    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j]), lo, d, 0, 0, 0);
-    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j]), hi, d, 0, 0, 0);
+#pragma unroll
+    for (int q = kAdapterParts - 1; q >= 0; --q) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ad_vec(bw[j]), h[q], d, 0, 0, 0);
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       o[2 * j + e] = f32_to_bf16_rne(bf16_lo(old[2 * j + e]) + d[2 * e]) |

@@ -148,7 +148,7 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
     }
     if (down > 0) hipLaunchKernelGGL(adapter_down_kernel, dim3((unsigned)down), block, 0, stream, a);
     auto launch_up = [&](auto kernel, int32_t row) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)up), block, (size_t)lds_rows * row * 2 * sizeof(uint16_t), stream, a, lds_rows);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)up), block, (size_t)lds_rows * row * kAdapterParts * sizeof(uint16_t), stream, a, lds_rows);
     };
     if (max_rank <= 32) launch_up(adapter_up_kernel<1>, adapter_row<1>());
     else if (max_rank <= 64) launch_up(adapter_up_kernel<2>, adapter_row<2>());

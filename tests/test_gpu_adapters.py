@@ -149,6 +149,29 @@ def test_infinities_of_b(rows, in_dim, part_dims, rank, accumulate):
     assert np.isinf(o).any() and np.isnan(o[:-1]).any() and np.isnan(o[-1]).sum() == 4
 
 
+@pytest.mark.parametrize("rows", [16, 64])
+@pytest.mark.parametrize("in_dim,rank", [(8, 8), (136, 16), (40, 104)])
+def test_products_of_x_and_a_keep_fp32(rows, in_dim, rank):
+    """x . A^T is held in fp32, not rounded below it: two rows of A, one 3 times the other,
+    against columns b and -3 b of B sum to exactly 0, and what comes out instead is off by
+    fp32's roundings alone.  All else of A, B is 0 and adds exactly, so those are 4 additions
+    of x . A^T, the scale, the two that part it and 6 of the last sum, each at most 2^-23
+    of the sum of magnitudes.  One rounding to 16 bits would be up to 2^-16 of a term."""
+    out, rng = 512, np.random.default_rng(in_dim * rank)
+    few = lambda *s: rng.integers(1, 32, s) * rng.choice([-1.0, 1.0], s) / 16.0  # noqa: E731  (5 bits, 3 times it 7)
+    a, b = np.zeros((rank, in_dim)), np.zeros((out, rank))
+    a[rank - 1, in_dim - 4:], b[:, rank - 2] = few(4), few(out)
+    a[rank - 2], b[:, rank - 1] = 3 * a[rank - 1], -3 * b[:, rank - 2]
+    t = lambda v: torch.from_numpy(v.astype(np.float32)).cuda().bfloat16()  # noqa: E731
+    x, a, b = t(rng.standard_normal((rows, in_dim))), [t(a)], [t(b)]
+    scales, y = [float(np.float32(1.37))], torch.empty(rows, out, device="cuda", dtype=torch.bfloat16)
+    Gemm().linear_adapters(x, Adapters(a, b, scales), [0] * rows, y)
+    mag = 1.37 * (np.abs(val(x)) @ np.abs(val(a[0])).T) @ np.abs(val(b[0])).T
+    err = np.abs(val(y)) / (13 * 2.0 ** -23 * mag)
+    print(f"[adapters] in {in_dim} rank {rank}: {err.max():.3g} of the tolerance", flush=True)
+    assert err.max() <= 1
+
+
 def test_beside_a_packed_projection_in_a_hip_graph():
     """The projection and its adapters captured and replayed, other work between the replays."""
     rng = np.random.default_rng(8)
