@@ -290,7 +290,7 @@ size_t baton_decode_attn_workspace_bytes(const baton_cache* cache);
  * are skipped, never read into arithmetic.  Free slots: nothing appended, out
  * rows set to 0.  Arithmetic in fp32; out rounded to nearest-even in the
  * cache's dtype (bf16 over a cache in 4 bits, where the softmax weights are
- * rounded to bf16 for their product with the values, their sum in fp32).
+ * rounded to 16 bits for their product with the values, their sum in fp32).
  * Live rows' holes are skipped like placeholders.
  * q, out: device [batch][n_q_heads][head_dim]; k_new, v_new: device
  * [batch][n_kv_heads][head_dim]; all 16-byte aligned.

@@ -21,17 +21,22 @@
 //    lane.  The codes are staged in LDS as they come, and the transposing read of
 //    4-bit elements hands lane i of a group of 16 the i-th column of 16 rows; the
 //    rows are given in the order of the lane's own scores, so one read per 16
-//    columns feeds two matrix operations.  A value's scale belongs to its token and its
+//    columns feeds both halves of the tokens.  A value's scale belongs to its token and its
 //    block of 32 columns, so it cannot be applied to operand pairs of two tokens:
-//    it multiplies the weight instead, P' = p 2^(s - 127), exact apart from the
-//    one rounding of p to bf16.  That makes P' differ between the column blocks --
+//    it multiplies the weight instead, P' = p 2^(s - 127), exactly.
+//    That makes P' differ between the column blocks --
 //    and a 16-column operand has columns to spare: with G query heads per kv-head,
 //    REP = min(D / 32, 16 / G) columns per head each carry another block, and of the
 //    16 result columns only the one with the slice's block is kept (at G = 8 and
 //    head_dim 128 two blocks share a column and P' is formed twice).
-// Weights are rounded to bf16 for the product (at most 2^-8 of each); their sum is
-// taken in fp32 before that rounding.
-// Registers are capped for three waves per SIMD (166 used); for four they spill, and
+//  * a weight is taken in two bf16 parts, which keep 16 bits of it (with one, the
+//    outputs of a step of random values were off by 0.0020 of their size, where their own
+//    rounding makes 0.0017).  Where 8 columns or fewer carry weights, the other 8 carry the
+//    second parts, and the two results are added once, at the item's end; else the second
+//    parts take matrix operations of their own.  A whole step takes 0.7 us longer than with
+//    one part at G = 1 (56.6), 1.3 and 5 at G = 8 (36.2 and 155: 32 and 61 rows, as above).
+// The weights' sum is taken in fp32 before they are parted.
+// Registers are capped for three waves per SIMD (up to 166 used); for four they spill, and
 // the kernel takes 1.5 to 2 times as long.
 // The step's own key and value take part as given, in bf16, and are stored in 4 bits.
 #pragma once
@@ -86,6 +91,7 @@ attn_kv4_kernel(const AttnArgs a) {
   constexpr int KK = Geo::kKk, DT = Geo::kDt, NB = Geo::kNb, VPT = D / 8, REC = D + 4;
   constexpr int REP = NB < 16 / G ? NB : 16 / G;   // columns per query head
   constexpr int NS = NB / REP;                     // blocks per column
+  constexpr bool SPARE = G * REP <= 8;             // columns 8 .. 15 carry the weights' second parts
   __shared__ __attribute__((aligned(16))) uint8_t lds_v[NW][Geo::kLdsV];
   __shared__ __attribute__((aligned(16))) float lds_s[NW][NB * 64];
   __shared__ float sm_m[NW][G], sm_l[NW][G];
@@ -95,7 +101,9 @@ attn_kv4_kernel(const AttnArgs a) {
   const int tid = threadIdx.x;
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave;
   const int g4 = lane / 16, c16 = lane % 16;
-  const int head = c16 / REP, hb = c16 % REP;      // this column's head (none from G on) and place
+  const int col8 = SPARE ? c16 % 8 : c16;
+  const bool rest = SPARE && c16 >= 8;
+  const int head = col8 / REP, hb = col8 % REP;    // this column's head (none from G on) and place
   uint8_t* lds = lds_v[w];
   float* ldss = lds_s[w];
 
@@ -236,23 +244,42 @@ attn_kv4_kernel(const AttnArgs a) {
       p[e] = fast_exp2(fmaf(s[e], qs, -ref));
       lsum += p[e];
     }
-    // P' operands: [set][half of the tokens]
-    bf16x8 pb[NS][2];
+    // The second part is what the first one's rounding (SPARE; else its cutting off) leaves.
+    if constexpr (SPARE) {
 #pragma unroll
-    for (int t = 0; t < NS; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x4 sc = *reinterpret_cast<const f32x4*>(ldss + (hb * NS + t) * 64 + 16 * j + 4 * g4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) pb[t][j / 2][4 * (j % 2) + r] = (__bf16)(p[4 * j + r] * sc[r]);
-      }
+      for (int e = 0; e < 16; ++e) p[e] = fmaf(rest ? -1.f : 0.f, (float)(__bf16)p[e], p[e]);
+    }
     const uint8_t* vt = lds + (16 * (c16 / 4) + 4 * g4 + c16 % 4) * Geo::kLdsRow;
+    // P' operands: [part][set], for the tokens of tiles 0 and 1, then of 2 and 3
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const i32x2_t c = read_tr4(vt + dt * 8);
-      const int t = (dt / 2) % NS;
-      o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(mx_widen(c[0], 1.f)), pb[t][0], o[dt], 0, 0, 0);
-      o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(mx_widen(c[1], 1.f)), pb[t][1], o[dt], 0, 0, 0);
+    for (int th = 0; th < 2; ++th) {
+      constexpr int NP = SPARE ? 1 : 2;
+      bf16x8 pb[NP][NS];
+#pragma unroll
+      for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const f32x4 sc = *reinterpret_cast<const f32x4*>(ldss + (hb * NS + t) * 64 + 16 * (2 * th + j) + 4 * g4);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float w = p[4 * (2 * th + j) + r];
+            if constexpr (SPARE) {
+              pb[0][t][4 * j + r] = (__bf16)(w * sc[r]);
+            } else {
+              const float first = __uint_as_float(__float_as_uint(w) & 0xFFFF0000u);
+              pb[0][t][4 * j + r] = (__bf16)(first * sc[r]);
+              pb[1][t][4 * j + r] = (__bf16)((w - first) * sc[r]);
+            }
+          }
+        }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const i32x2_t c = read_tr4(vt + dt * 8);
+        const bf16x8 v = as_bf16x8(mx_widen(c[th], 1.f));
+#pragma unroll
+        for (int h2 = 0; h2 < NP; ++h2)
+          o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pb[h2][(dt / 2) % NS], o[dt], 0, 0, 0);
+      }
     }
   };
 
@@ -312,13 +339,16 @@ attn_kv4_kernel(const AttnArgs a) {
     const float p = fast_exp2(s - ref);
     lsum = lsum * f + p;
     m = mx;
+    // its two parts (the second not 0, so that an infinite value meets one sign alone)
+    const float first = __uint_as_float(__float_as_uint(p) & 0xFFFF0000u);
+    const float second = __uint_as_float(__float_as_uint(p) | 1u) - first;
     bf16x8 pa;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) pa[e] = (__bf16)(e == 0 ? p : 0.f);
+    for (int e = 0; e < 8; ++e) pa[e] = (__bf16)(e == 0 ? (rest ? second : first) : e == 1 && !SPARE ? second : 0.f);
     const uint16_t* v16 = reinterpret_cast<const uint16_t*>(vnew);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      const u32x4 vw = {g4 == 0 ? (uint32_t)v16[16 * dt + c16] : 0u, 0u, 0u, 0u};
+      const u32x4 vw = {g4 == 0 ? (uint32_t)v16[16 * dt + c16] * (SPARE ? 1u : 0x10001u) : 0u, 0u, 0u, 0u};
       o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vw), pa, o[dt] * f, 0, 0, 0);
     }
     const bool is_v = lane >= VPT;
@@ -337,7 +367,14 @@ attn_kv4_kernel(const AttnArgs a) {
   // 16 dt + 4 (l / 16) + r of its head.
   lsum = sum_over_groups(lsum);
   __builtin_amdgcn_wave_barrier();
-  if (head < G) {
+  if constexpr (SPARE) {      // both parts' products added
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        o[dt][r] += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(o[dt][r]), 0x128, 0xF, 0xF, true));   // row_ror 8
+  }
+  if (head < G && !rest) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
       if (dt / 2 / NS == hb) *reinterpret_cast<f32x4*>(lds + (head * D + 16 * dt + 4 * g4) * 4) = o[dt];

@@ -165,6 +165,41 @@ def test_rows_around_the_block_edges(shape):
     print(f"[kv4] {shape}: {p.worst:.3g} of the tolerance", flush=True)
 
 
+@pytest.mark.parametrize("shape", [(1, 1, 4, 4, 64), (1, 1, 8, 4, 64), (1, 1, 16, 4, 64), (1, 1, 16, 2, 64),
+                                   (1, 1, 4, 4, 128), (1, 1, 4, 2, 128), (1, 1, 8, 2, 128), (1, 1, 16, 2, 128)], ids=_sid)
+def test_weights_are_kept_past_bf16(shape):
+    """Sums of a few values that nearly cancel: the softmax weights are rounded no more
+    than to 2^-16 of each, so beside the output's own rounding an element is off by
+    that and the 2^-13 of fp32 arithmetic times sum p |v| / sum p."""
+    layers, _, hq, hkv, d = shape
+    lens = [1 + b % 29 for b in range(58)] + [300, 64]
+    p = Pair(layers, len(lens), hq, hkv, d, 320, seed=hq, split=128)
+    p.embed(list(range(len(lens))), lens)
+    q, k, v = (p.draw(layers, len(lens), 1, h, d) for h in (hq, hkv, hkv))
+    got = val(p.c.decode_attn(0, *(bf16(x[0, :, 0]) for x in (q, k, v))))
+    worst = 0.0
+    for (_, b, _), (o, a) in p.m.step(q, k, v).items():
+        err = np.abs(got[b] - o) / (2.0 ** -8 * np.abs(o) + (2.0 ** -16 + 2.0 ** -13) * a + 1e-30)
+        worst = max(worst, err.max())
+    print(f"[kv4] {shape}: {worst:.3g} of the tolerance", flush=True)
+    assert worst <= 1
+
+
+def test_an_infinite_value_of_the_step_itself():
+    """The step's own value takes part as given: an infinity comes out as one."""
+    for hq, hkv, d in ((2, 2, 64), (8, 1, 64), (2, 2, 128), (4, 2, 128), (4, 1, 128), (8, 1, 128)):
+        c = BatonCache(1, 3, hq, hkv, d, 48, dtype="mxfp4")
+        k, v = (torch.randn(1, hkv, 30, d, device="cuda").bfloat16() for _ in range(2))
+        c.embed([0, 2], [30, 30], [k, k], [v, v])
+        q, kn, vn = (torch.randn(3, h, d, device="cuda").bfloat16() for h in (hq, hkv, hkv))
+        vn[0, 0, 5], vn[0, 0, d - 1] = float("inf"), -float("inf")
+        out = c.decode_attn(0, q, kn, vn)
+        g = hq // hkv
+        assert (out[0, :g, 5] == float("inf")).all() and (out[0, :g, d - 1] == -float("inf")).all()
+        out[0, :g, 5] = out[0, :g, d - 1] = 0.0
+        assert out.isfinite().all()
+
+
 @pytest.mark.parametrize("shape", SHAPES, ids=_sid)
 @pytest.mark.parametrize("layout", ["by_layer", "separate"])
 def test_story(shape, layout):
