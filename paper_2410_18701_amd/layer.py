@@ -130,7 +130,7 @@ class Gemm:
         for t in (x, y):
             if not t.is_contiguous() or t.dtype != torch.bfloat16:
                 raise ValueError("linear_adapters: contiguous bf16 tensors only")
-        _on_this_gpu("linear_adapters", x, y, *adapters.a[:1])
+        _on_this_gpu("linear_adapters", x, y, self.ws, *adapters.a[:1])
         B.baton_linear_adapters(B.BATON_BF16, x, adapters.table, adapters.n, row_adapter, y, rows, y.shape[1], in_dim,
                                 adapters.parts, 1 if adapters.parts is None else len(adapters.parts), accumulate,
                                 self.ws, self.ws_bytes, _stream())

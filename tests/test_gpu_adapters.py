@@ -210,3 +210,13 @@ def test_calls_follow_the_current_stream():
     torch.cuda.current_stream().wait_stream(side)
     o, tol = want(x, a, b, scales, [0] * 8, [64], y, False)
     assert (np.abs(val(got) - o) <= tol).all()
+
+
+def test_a_workspace_elsewhere_is_refused():
+    """A workspace that is not on the current device, as a Gemm made on another one has."""
+    rng = np.random.default_rng(1)
+    x, a, b, scales, y = make(rng, 4, 64, [32], [8])
+    g = Gemm()
+    g.ws = torch.empty(g.ws_bytes, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="current device"):
+        g.linear_adapters(x, Adapters(a, b, scales), [0] * 4, y)
