@@ -43,7 +43,7 @@ class Adapters:
             raise ValueError("Adapters: a, b and scales need the same length")
         self.a, self.b, self.n = list(a), list(b), len(a)
         self.parts = None if parts is None else (ctypes.c_int32 * len(parts))(*[int(p) for p in parts])
-        n_parts = 1 if parts is None else len(self.parts)
+        n_parts = self.n_parts = 1 if parts is None else len(self.parts)
         self.max_rank = max((t.shape[1] for t in self.b), default=0)
         self.table = (B.baton_adapter * max(1, self.n))()
         for i, (ai, bi, s) in enumerate(zip(self.a, self.b, scales)):
@@ -130,10 +130,15 @@ class Gemm:
         for t in (x, y):
             if not t.is_contiguous() or t.dtype != torch.bfloat16:
                 raise ValueError("linear_adapters: contiguous bf16 tensors only")
+        if rows * adapters.n_parts * adapters.max_rank * 4 > self.ws_bytes:   # these rows may have smaller ranks
+            rank = max((adapters.b[i].shape[1] for i in row_adapter if 0 <= i < adapters.n), default=0)
+            need = B.baton_linear_adapters_workspace_bytes(rows, adapters.n_parts, rank)
+            if need > self.ws_bytes:
+                raise ValueError(f"linear_adapters: rank {rank} needs a workspace of {need} bytes, the Gemm has "
+                                 f"{self.ws_bytes}")
         _on_this_gpu("linear_adapters", x, y, self.ws, *adapters.a[:1])
         B.baton_linear_adapters(B.BATON_BF16, x, adapters.table, adapters.n, row_adapter, y, rows, y.shape[1], in_dim,
-                                adapters.parts, 1 if adapters.parts is None else len(adapters.parts), accumulate,
-                                self.ws, self.ws_bytes, _stream())
+                                adapters.parts, adapters.n_parts, accumulate, self.ws, self.ws_bytes, _stream())
         return y
 
     def close(self):

@@ -71,6 +71,20 @@ def test_adapters_wrapper_refusals():
             bad()
 
 
+def test_adapters_too_small_a_workspace_is_named():
+    """Before the call, by the largest rank that a row uses (nothing is allocated or enqueued)."""
+    from paper_2410_18701_amd.layer import Gemm
+    t = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    ad = Adapters([t(16, 64), t(48, 64)], [t(32, 8), t(32, 24)], [1.0, 1.0], parts=[8, 24])
+    g, x, y = Gemm(0), t(3, 64), t(3, 32)
+    g.ws_bytes = 4 * 3 * 2 * 24 - 1
+    with pytest.raises(ValueError, match="rank 24 needs a workspace of 576 bytes, the Gemm has 575"):
+        g.linear_adapters(x, ad, [0, 1, -1], y)
+    with pytest.raises(Exception) as e:          # rank 8 alone fits: refused for the tensors' device, not the workspace
+        g.linear_adapters(x, ad, [0, 0, -1], y)
+    assert "workspace" not in str(e.value)
+
+
 def sample_status(dtype=B.BATON_BF16, logits=X, ld=100, rows=4, vocab=100, temperature=0, top_k=0, top_p=0, min_p=0,
                   u=W, tokens=Y):
     try:
