@@ -382,7 +382,8 @@ baton_status baton_cache_tokens(const baton_cache* cache, int32_t* tokens);
  * Tuning: tokens per split of a row in baton_decode_attn, i.e. per work item
  * (one workgroup; a multiple of 64, 64 .. 4096), or 0 (the default) to let
  * each step choose from its total number of cached tokens (256 .. 4096, about
- * 4096 items per layer).  Changes
+ * 4096 items per layer; over a cache in 4 bits, whose tokens cost a quarter as
+ * much, from its longest row too, and fewer items).  Changes
  * baton_decode_attn_workspace_bytes; only between steps.
  * Errors: EINVAL (out of range), ESTATE (inside a decode step).
  */

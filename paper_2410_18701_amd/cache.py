@@ -50,7 +50,8 @@ class BatonCache:
 
     k, v: [n_layers][batch][n_kv_heads][capacity][head_dim] device tensors,
     each layer dense; with dtype "mxfp4" (held in 4 bits, sources, queries and
-    outputs bf16) [n_layers][batch][n_kv_heads][row_bytes_mxfp4] bytes.  Unless given, they are made with layout "by_layer" --
+    outputs bf16; capacity a multiple of 16) [n_layers][batch][n_kv_heads][row_bytes_mxfp4]
+    bytes.  Unless given, they are made with layout "by_layer" --
     views of one [n_layers][2][batch][n_kv_heads][capacity][head_dim] tensor,
     K and V of a layer next to each other (the library streams them about 4%
     faster than from two allocations) -- or "separate" (two tensors).

@@ -18,7 +18,7 @@
 //    turns one rounding of y in some 250 the other way.
 // Sums are fp32 in a fixed order: the same call gives the same bits.
 // us down / up: 64 rows of 24 adapters of rank 32, 4096 to 3 parts of 4096 (35 MB)
-// 7.0 / 8.2; 240 rows of 40 of rank 64, 4096 to 2 of 11008 (177 MB with y) 15.4 / 32.7.
+// 7.0 / 8.3; 240 rows of 40 of rank 64, 4096 to 2 of 11008 (177 MB with y) 15.0 / 32.3.
 #pragma once
 
 #include <type_traits>

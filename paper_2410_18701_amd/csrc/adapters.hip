@@ -119,9 +119,10 @@ baton_status baton_linear_adapters(int32_t dtype, const void* x, const baton_ada
       if (hipGetLastError() != hipSuccess) return BATON_EHIP;
       continue;
     }
-    // Ranges of k: 1024 workgroups in all or a few more, at least eight steps of 32
-    // (the loads a wave has in flight at once) for each wave.  us of both launches, 256
-    // rows of 40 adapters of rank 64, 4096 to 2 x 11008: with 512 workgroups 53.7, with
+    // Ranges of k: 1024 workgroups in all or a few more, at most one range for every 1024
+    // columns begun -- eight steps of 32 (the loads a wave has in flight at once) for each
+    // of four waves at a multiple of 1024, five at least past the first.  us of both
+    // launches, 256 rows of 40 adapters of rank 64, 4096 to 2 x 11008: with 512 workgroups 53.7, with
     // 1024 50.2; 64 rows of 24 of rank 32, 4096 to 12288: 15.3, with four steps a wave 16.3.
     const int64_t fit = per_split ? (int64_t)(ws_bytes / per_split) : 1;
     int64_t splits = units > 0 ? (1024 + units - 1) / units : 1;

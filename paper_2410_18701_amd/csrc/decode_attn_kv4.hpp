@@ -5,10 +5,11 @@
 // What bounds it is HBM -- 68 bytes of K or V per token at head_dim 128, against
 // 256 in bf16 -- as long as turning codes into operands costs few instructions,
 // and then each item's start (its descriptor, the query, the first loads) and end:
-// 37 us for 152 MB (32 rows of up to 2048 tokens, 32 heads; 4.1 TB/s), 59 for 295 MB
-// (61 rows of up to 8192, 64 heads over 8; 5.0), where a copy of it that only loads
+// 39 us for 152 MB (32 rows of up to 2048 tokens, 32 heads; 3.9 TB/s), 62 for 295 MB
+// (61 rows of up to 8192, 64 heads over 8; 4.8), where a copy of it that only loads
 // takes 32 and 54 and a plain read of as many bytes 23 and 42.  The vector ALUs are
-// active 49% of the time, the matrix cores 12%.  Per iteration a wave takes 64 tokens:
+// active 36% and 45% of the launch, the matrix cores 11% and 18%.  Per iteration a wave
+// takes 64 tokens:
 //  * QK^T: A = 16 key rows x 32 of d, four tiles of 16 consecutive tokens.  The
 //    contraction's order is free, so lane l takes the D / 4 elements from D / 4 *
 //    (l / 16) on of its key row -- one load of 16 bytes (8 at head_dim 64), a

@@ -116,9 +116,9 @@ baton_status append_prompts4(const baton_cache* c, const baton::PrefillArgs& p, 
 // CU can, so an item per CU is enough (tokens / 256); and a row of n tokens in n / S
 // pieces pays for each piece in the work list and the merge, about 0.25 us a
 // piece, against 2 ns per token of an item, balanced at S = sqrt(128 n).  us per
-// layer at S and at 256 tokens: one row of 32,768 over one kv-head 23.5 (2048) and
-// 42.9, of 100,000 over eight 36 (3584) and 131, of 8192 over 32 18.7 (1024) and
-// 26.9; 32 rows of up to 2048 over 32 38.7 (4096) and 52.6.
+// layer at S and at 256 tokens: one row of 32,768 over one kv-head 24.4 (2048) and
+// 43.3, of 100,000 over eight 39 (3584) and 132, of 8192 over 32 18.5 (1024) and
+// 27.4; 32 rows of up to 2048 over 32 40.0 (4096) and 53.2.
 int32_t kv4_split(const baton_cache* c) {
   const baton::HoleList hl = hole_list(c);
   int64_t total = 0, longest = 0;

@@ -17,9 +17,11 @@
 // One workgroup of 16 waves per row.  The row is read once from memory into LDS (what
 // does not fit is read again); wave w owns the w-th of 16 contiguous parts of
 // it, 16 bytes per lane and step.  What bounds it is the vector ALUs of one compute
-// unit -- a weight takes about 25 instructions, a row of 32,000 all weighed 5 us --
-// and the latency of its dependent steps, so whole passes over the row are kept few
-// and a list of tokens in LDS takes their place as soon as one can:
+// unit -- a weight takes about 25 instructions, a row of 32,000 all weighed 5 us; they
+// are active 64 to 69% of the time that a row takes -- and the latency of its dependent
+// steps, so whole passes over the row are kept few and a list of tokens in LDS takes
+// their place as soon as one can.  With a row per compute unit the launch then waits for
+// the slowest one (256 rows of 128,000 that differ: a unit is busy 31 of 79 us):
 //  * top_k up to 512: the k-th largest of the threads' own largest values bounds
 //    the k-th largest from below (up to 1024, counts in bins of the values do); the
 //    tokens from there on, a few more than k, are the list.

@@ -217,7 +217,8 @@ class DecodeLayers:
     adapters[layer]: dict from names of PROJ to Adapters (qkv in parts [Hq D, Hkv D,
     Hkv D], gate_up in [F, F], the same adapter at the same index everywhere);
     slot_adapter[slot] is the index its query uses, -1 for none, and may be changed
-    between steps (a captured step keeps the indices that it was captured with).  head: dict of norm [hid] and out [vocab][hid], for next_tokens."""
+    between steps (a captured step keeps the indices that it was captured with).  head: dict
+    of norm [hid] and out [vocab][hid] (vocab a multiple of 8), for next_tokens."""
 
     PROJ = ("qkv", "o", "gate_up", "down")
 
