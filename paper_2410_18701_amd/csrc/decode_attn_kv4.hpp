@@ -35,7 +35,8 @@
 //    rounding makes 0.0017).  Where 8 columns or fewer carry weights, the other 8 carry the
 //    second parts, and the two results are added once, at the item's end; else the second
 //    parts take matrix operations of their own.  A whole step takes 0.7 us longer than with
-//    one part at G = 1 (56.6), 1.3 and 5 at G = 8 (36.2 and 155: 32 and 61 rows, as above).
+//    one part at G = 1 (56.7), at G = 8 1.4 (36.3, 32 rows of up to 32,768) and 5 (155, two
+//    layers of the 61 rows above).
 // The weights' sum is taken in fp32 before they are parted.
 // Registers are capped for three waves per SIMD (up to 166 used); for four they spill, and
 // the kernel takes 1.5 to 2 times as long.
