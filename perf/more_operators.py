@@ -441,7 +441,7 @@ def run(s):
         _begin(cache, s["none"], s["keep"])
         return ks, vs, table
     if own:
-        return [cache.decode_attn(l, s["q"][l], s["k_new"][l], s["v_new"][l], n_new=s["n_new"], out=s["out"][l])
+        return [cache.decode_attn(l, s["q"][l], s["k_new"][l], s["v_new"][l], out=s["out"][l])
                 for l in range(c["layers"])]
     return [_attention(cache, l, s["q"][l], s["k_new"][l], s["v_new"][l], s["map"], s["n_new"], c["window"], c["sinks"])
             for l in range(c["layers"])]
