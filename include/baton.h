@@ -579,6 +579,142 @@ baton_status baton_sample(int32_t dtype, const void* logits, int64_t ld, int32_t
                           const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                           const float* u, int32_t* tokens, hipStream_t stream);
 
+/*
+ * ---- A cache in pages, for steps with drafted tokens ------------------------
+ *
+ * Beside the aligned ring: keys and values in pages of a pool that all slots share,
+ * with each slot's length and table of pages in device memory.  A step takes from one
+ * to BATON_PAGED_MAX_WIDTH new tokens per slot -- the next one and drafted ones behind
+ * it -- and how many of them stay is known on the GPU alone (baton_verify), so that
+ * whole steps are enqueued, or captured into a graph, without waiting for the host.
+ *
+ * A step: baton_paged_step (ends the last step, hands out pages), then for each layer
+ * baton_paged_attn, then e.g. baton_verify, whose n_out is the next step's keep.
+ *
+ * With window > 0 a new token at position p sees the tokens j with p - window < j <= p
+ * and those with j < sinks (the first tokens stay visible), else all j <= p.  Pages
+ * that no later token can see go back to the pool.  Positions count all tokens of a
+ * query.
+ *
+ * All memory is the caller's; the library keeps nothing.  Work on one cache goes to one
+ * stream.  k, v: [n_layers][n_pages][n_kv_heads][page * head_dim] elements; the order
+ * within a page is the library's own (baton_paged_embed and baton_paged_extract take
+ * and give rows).  table: [batch][max_pages], entry j the page of tokens j page .. ,
+ * -1 where there is none; lens: [batch], tokens of each slot, 0 of a free one; state:
+ * baton_paged_state_bytes, the library's.  baton_paged_reset before anything else;
+ * after that table, lens and state are for the caller to read only.
+ */
+#define BATON_PAGED_MAX_WIDTH 16 /* new tokens of a slot in a step */
+#define BATON_PAGED_MAX_ROWS 64  /* new tokens times query heads per kv-head */
+
+typedef struct baton_paged_desc {
+  int32_t dtype;      /* BATON_F32 or BATON_BF16: of K, V, sources, q, k_new, v_new and out */
+  int32_t n_layers;   /* >= 1 */
+  int32_t batch;      /* slots, 1 .. BATON_MAX_BATCH */
+  int32_t n_q_heads;  /* query heads per layer */
+  int32_t n_kv_heads; /* key/value heads per layer (n_q_heads / n_kv_heads in {1,2,4,8}) */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t page;       /* tokens per page: 32, 64, 128 or 256 */
+  int32_t n_pages;    /* pages of the pool; n_pages * page < 2^31 */
+  int32_t max_pages;  /* a slot's table entries, 1 .. 2^20 */
+  int32_t window;     /* 0: none */
+  int32_t sinks;      /* first tokens that stay visible beside a window */
+  void* k;            /* device, 16-byte aligned */
+  void* v;            /* device, as k */
+  int64_t layer_stride; /* elements from layer to layer, in k and v alike; 0: packed; else as
+                           baton_cache_desc's */
+  int32_t* table;     /* device [batch][max_pages] */
+  int32_t* lens;      /* device [batch] */
+  int32_t* state;     /* device, 16-byte aligned */
+} baton_paged_desc;
+
+/* Bytes of `state` (by the sizes alone, the pointers are not looked at); 0 for sizes out of range. */
+size_t baton_paged_state_bytes(const baton_paged_desc* desc);
+
+/*
+ * An empty cache: every slot free, every page in the pool.  order: device array of
+ * n_pages, a permutation of 0 .. n_pages - 1, the order in which pages are taken, or
+ * NULL (0, 1, ...).  K and V are not written.
+ * Errors of this and every call with a descriptor: EINVAL (null or misaligned pointer,
+ * sizes out of range, layers that overlap), EDTYPE (dtype, head_dim or grouping
+ * unsupported), EHIP.
+ */
+baton_status baton_paged_reset(const baton_paged_desc* desc, const int32_t* order, hipStream_t stream);
+
+/*
+ * Ends the last step and begins the next.  keep, n_new: device arrays of batch entries.
+ * Of slot b's tokens those stay that it had before the last step and the first keep[b]
+ * of that step's new ones (NULL: none of them); keep[b] < 0: its query leaves, the slot is free, its
+ * pages go back.  Then n_new[b] new tokens (< 1: none) are provided for: pages for
+ * lens[b] + n_new[b] tokens in all are in the table, pages past that go back to the
+ * pool (what was drafted and not kept), and so do those behind the window.
+ * Pages go back before any are taken, and are taken by the slots in order: a slot
+ * whose need, with that of all slots in front of it, exceeds the pool, or whose tokens
+ * exceed its table, gets none and takes no part in the step (nothing of it is appended
+ * or written to out).  missing (device, [batch], or NULL) gets the pages it lacks, 0 of
+ * the other slots.  slot_map (device, [batch] rows of map_ld, or NULL): for i < width
+ * the place page id * page + offset of the slot's i-th new token, -1 past the last.
+ * The same calls give the same tables: pages are a stack, those given back lie in
+ * order of (slot, block) from its top, and the k-th one taken, in the same order, is
+ * the k-th from the top.  A prompt is a step too: n_new its length, then
+ * baton_paged_embed; attention leaves slots with more than its width alone.
+ * Errors: EINVAL also for null n_new, width outside 1 .. 2^20 or map_ld < width with a slot_map.
+ */
+baton_status baton_paged_step(const baton_paged_desc* desc, const int32_t* keep, const int32_t* n_new,
+                              int32_t* slot_map, int32_t width, int64_t map_ld, int32_t* missing, hipStream_t stream);
+
+/*
+ * Whole queries into their slots' pages, and out of them.  slots, lens: host arrays of
+ * n entries (distinct slots; lens[i] the query's tokens); k_src .. v_dst: host arrays of
+ * n device pointers, each [n_layers][n_kv_heads][lens[i]][head_dim] contiguous, 16-byte
+ * aligned -- what baton_kv_embed takes and baton_kv_extract gives.  Embed writes tokens
+ * 0 .. lens[i] - 1, in the step whose n_new is the query's length (what the slot's pages
+ * hold behind them is not kept); extract reads them.  Tokens without a page are
+ * left out.
+ * Errors: EINVAL also for n < 0, a slot out of range or listed twice, lens[i] outside
+ * 1 .. max_pages * page.
+ */
+baton_status baton_paged_embed(const baton_paged_desc* desc, const int32_t* slots, int32_t n, const int32_t* lens,
+                               const void* const* k_src, const void* const* v_src, hipStream_t stream);
+baton_status baton_paged_extract(const baton_paged_desc* desc, const int32_t* slots, int32_t n, const int32_t* lens,
+                                 void* const* k_dst, void* const* v_dst, hipStream_t stream);
+
+/*
+ * baton_rope_qkv for `width` new tokens per slot: qkv device [batch][width][(n_q_heads
+ * + 2 n_kv_heads) head_dim], q, k_new, v_new [batch][width][heads][head_dim]; row i of
+ * slot b is rotated for position lens[b] + i.  bf16.
+ * Errors: EINVAL also for theta <= 1, width outside 1 .. BATON_PAGED_MAX_WIDTH.
+ */
+baton_status baton_paged_rope_qkv(const baton_paged_desc* desc, const void* qkv, int32_t width, void* q, void* k_new,
+                                  void* v_new, float theta, hipStream_t stream);
+
+/* Bytes of device workspace that baton_paged_attn needs; 0 where no slot's tokens are
+   ever divided, and for sizes out of range. */
+size_t baton_paged_attn_workspace_bytes(const baton_paged_desc* desc, int32_t width);
+
+/*
+ * Attention of the step's new tokens in one layer.  k_new[b][i], v_new[b][i] (device
+ * [batch][width][n_kv_heads][head_dim], or both NULL: they are in the pages) go to the
+ * place of slot b's i-th new token, and for each of its query heads
+ *     out[b][i] = softmax_j(scale * q[b][i] . K_j) . V_j
+ * over the tokens j that it sees (above), its own among them.  q, out: device
+ * [batch][width][n_q_heads][head_dim].  Rows of out past a slot's new tokens are not
+ * written.  What a token does not see -- the tokens behind it, those outside the
+ * window, what else its pages hold -- has no influence, whatever its bits.  fp32
+ * arithmetic (bf16: softmax weights have 16 bits for their product with the values,
+ * 8 in blocks of 32 tokens with infinite or NaN values), out rounded to nearest even.
+ * scale = 0 selects 1/sqrt(head_dim).  A step may be repeated: the same calls give the
+ * same bits.
+ * ws: baton_paged_attn_workspace_bytes, 16-byte aligned; nothing is kept there between
+ * calls, but calls that share one go to one stream.
+ * Errors: EINVAL also for a layer out of range, one of k_new and v_new alone, a
+ * misaligned pointer, width outside 1 .. BATON_PAGED_MAX_WIDTH or width * n_q_heads / n_kv_heads >
+ * BATON_PAGED_MAX_ROWS, a scale that is not finite, ws too small.
+ */
+baton_status baton_paged_attn(const baton_paged_desc* desc, int32_t layer, const void* q, const void* k_new,
+                              const void* v_new, int32_t width, void* out, float scale, void* ws, size_t ws_bytes,
+                              hipStream_t stream);
+
 /* Static English text of a status. */
 const char* baton_status_string(baton_status status);
 

@@ -20,6 +20,8 @@ BATON_SCRATCH_BYTES = 64 << 20
 BATON_GEMM_MAX_ROWS = 256
 BATON_ADAPTER_MAX_RANK = 128
 BATON_ADAPTER_MAX_PARTS = 4
+BATON_PAGED_MAX_WIDTH = 16
+BATON_PAGED_MAX_ROWS = 64
 BATON_F32, BATON_BF16, BATON_MXFP4 = 0, 1, 2
 BATON_FILL_NEG_INF_F32 = 0xFF800000
 BATON_FILL_NEG_INF_BF16 = 0xFF80
@@ -43,6 +45,13 @@ class baton_cache_desc(ctypes.Structure):
 class baton_adapter(ctypes.Structure):
     _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("rank", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class baton_paged_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_layers", "batch", "n_q_heads", "n_kv_heads", "head_dim",
+                                              "page", "n_pages", "max_pages", "window", "sinks")] + \
+               [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("state", ctypes.c_void_p)]
 
 
 class BatonError(RuntimeError):
@@ -97,6 +106,17 @@ def lib():
         L.baton_linear_adapters.argtypes = [i32, vp, P(baton_adapter), i32, P(i32), vp, i32, i32, i32, P(i32), i32,
                                             i32, vp, ctypes.c_size_t, vp]
         L.baton_sample.argtypes = [i32, vp, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        pd, sz = P(baton_paged_desc), ctypes.c_size_t
+        L.baton_paged_state_bytes.argtypes = [pd]
+        L.baton_paged_state_bytes.restype = sz
+        L.baton_paged_reset.argtypes = [pd, vp, vp]
+        L.baton_paged_step.argtypes = [pd, vp, vp, vp, i32, i64, vp, vp]
+        L.baton_paged_embed.argtypes = [pd, P(i32), i32, P(i32), P(vp), P(vp), vp]
+        L.baton_paged_extract.argtypes = [pd, P(i32), i32, P(i32), P(vp), P(vp), vp]
+        L.baton_paged_rope_qkv.argtypes = [pd, vp, i32, vp, vp, vp, ctypes.c_float, vp]
+        L.baton_paged_attn_workspace_bytes.argtypes = [pd, i32]
+        L.baton_paged_attn_workspace_bytes.restype = sz
+        L.baton_paged_attn.argtypes = [pd, i32, vp, vp, vp, i32, vp, ctypes.c_float, vp, sz, vp]
         L.baton_status_string.argtypes = [st]
         L.baton_status_string.restype = ctypes.c_char_p
         for name in ("baton_cache_create", "baton_cache_destroy", "baton_kv_evict", "baton_kv_embed",
@@ -105,7 +125,9 @@ def lib():
                      "baton_cache_query", "baton_set_split_tokens", "baton_cache_flush",
                      "baton_shape_insert", "baton_cache_tokens", "baton_kv_move", "baton_linear_pack", "baton_linear_packed",
                      "baton_linear_packed_rmsnorm", "baton_linear_packed_silu",
-                     "baton_rmsnorm", "baton_rope_qkv", "baton_silu_mul", "baton_linear_adapters", "baton_sample"):
+                     "baton_rmsnorm", "baton_rope_qkv", "baton_silu_mul", "baton_linear_adapters", "baton_sample",
+                     "baton_paged_reset", "baton_paged_step", "baton_paged_embed", "baton_paged_extract",
+                     "baton_paged_rope_qkv", "baton_paged_attn"):
             getattr(L, name).restype = st
         _lib = L
     return _lib
@@ -312,3 +334,49 @@ def baton_linear_adapters(dtype, x, adapters, n_adapters, row_adapter, y, rows, 
 def baton_sample(dtype, logits, ld, rows, vocab, temperature, top_k, top_p, min_p, u, tokens, stream=None):
     _check(lib().baton_sample(dtype, _ptr(logits), ld, rows, vocab, _ptr(temperature), _ptr(top_k), _ptr(top_p),
                               _ptr(min_p), _ptr(u), _ptr(tokens), _stream(stream)), "baton_sample")
+
+
+# ---- a cache in pages ----
+def baton_paged_state_bytes(desc):
+    return lib().baton_paged_state_bytes(ctypes.byref(desc))
+
+
+def baton_paged_reset(desc, order=None, stream=None):
+    _check(lib().baton_paged_reset(ctypes.byref(desc), _ptr(order), _stream(stream)), "baton_paged_reset")
+
+
+def baton_paged_step(desc, keep, n_new, slot_map=None, width=1, map_ld=1, missing=None, stream=None):
+    _check(lib().baton_paged_step(ctypes.byref(desc), _ptr(keep), _ptr(n_new), _ptr(slot_map), width, map_ld,
+                                  _ptr(missing), _stream(stream)), "baton_paged_step")
+
+
+def _paged_copy(call, desc, slots, lens, k, v, stream):
+    s_arr, n = _i32s(slots)
+    l_arr, nl = _i32s(lens)
+    if nl != n or len(k) != n or len(v) != n:
+        raise ValueError("slots, lens, keys and values must have the same length")
+    ks = (ctypes.c_void_p * max(1, n))(*[_ptr(x) for x in k])
+    vs = (ctypes.c_void_p * max(1, n))(*[_ptr(x) for x in v])
+    _check(getattr(lib(), call)(ctypes.byref(desc), s_arr, n, l_arr, ks, vs, _stream(stream)), call)
+
+
+def baton_paged_embed(desc, slots, lens, k_src, v_src, stream=None):
+    _paged_copy("baton_paged_embed", desc, slots, lens, k_src, v_src, stream)
+
+
+def baton_paged_extract(desc, slots, lens, k_dst, v_dst, stream=None):
+    _paged_copy("baton_paged_extract", desc, slots, lens, k_dst, v_dst, stream)
+
+
+def baton_paged_rope_qkv(desc, qkv, width, q, k_new, v_new, theta, stream=None):
+    _check(lib().baton_paged_rope_qkv(ctypes.byref(desc), _ptr(qkv), width, _ptr(q), _ptr(k_new), _ptr(v_new),
+                                      float(theta), _stream(stream)), "baton_paged_rope_qkv")
+
+
+def baton_paged_attn_workspace_bytes(desc, width):
+    return lib().baton_paged_attn_workspace_bytes(ctypes.byref(desc), width)
+
+
+def baton_paged_attn(desc, layer, q, k_new, v_new, width, out, scale, ws, ws_bytes, stream=None):
+    _check(lib().baton_paged_attn(ctypes.byref(desc), layer, _ptr(q), _ptr(k_new), _ptr(v_new), width, _ptr(out),
+                                  float(scale), _ptr(ws), ws_bytes, _stream(stream)), "baton_paged_attn")

@@ -906,14 +906,14 @@ baton_status baton_rope_qkv(const baton_cache* c, const void* qkv, void* q, void
   if (c->n_prefill) return BATON_ESTATE;   // decode steps only
   baton::RopeArgs a;
   std::memset(&a, 0, sizeof(a));
-  a.qkv = static_cast<const uint16_t*>(qkv);
-  a.q = static_cast<uint16_t*>(q);
-  a.k = static_cast<uint16_t*>(k_new);
-  a.v = static_cast<uint16_t*>(v_new);
-  a.n_q_heads = c->d.n_q_heads;
-  a.n_kv_heads = c->d.n_kv_heads;
-  a.head_dim = c->d.head_dim;
-  a.log2_theta = std::log2((double)theta);
+  a.shape.qkv = static_cast<const uint16_t*>(qkv);
+  a.shape.q = static_cast<uint16_t*>(q);
+  a.shape.k = static_cast<uint16_t*>(k_new);
+  a.shape.v = static_cast<uint16_t*>(v_new);
+  a.shape.n_q_heads = c->d.n_q_heads;
+  a.shape.n_kv_heads = c->d.n_kv_heads;
+  a.shape.head_dim = c->d.head_dim;
+  a.shape.log2_theta = std::log2((double)theta);
   const baton::HoleList hl = hole_list(c);
   for (int32_t b = 0; b < c->d.batch; ++b) a.pos[b] = row_tokens(c, b, hl);
   const int heads = c->d.n_q_heads + 2 * c->d.n_kv_heads;

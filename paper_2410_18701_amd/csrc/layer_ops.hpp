@@ -66,39 +66,56 @@ __global__ void __launch_bounds__(NT) rmsnorm_kernel(const u32x4* __restrict__ x
 // lane i < D/2 rotates pair (i, i + D/2) by pos_b * theta^(-2i/D).  The angle
 // is formed and reduced modulo 2 pi in double precision, its sine and cosine
 // then taken in single precision on [-pi, pi].
-struct RopeArgs {
+struct RopeShape {
   const uint16_t* qkv;
   uint16_t* q;
   uint16_t* k;
   uint16_t* v;
   int32_t n_q_heads, n_kv_heads, head_dim;
   double log2_theta;
+};
+
+struct RopeArgs {
+  RopeShape shape;
   int32_t pos[512];
 };
 
-__global__ void __launch_bounds__(kWave) rope_qkv_kernel(const RopeArgs a) {
+// Head `head` of input row `row`, whose token is at position `pos`.
+__device__ __forceinline__ void rope_head(const RopeShape& a, int64_t row, int head, int32_t pos) {
   const int hq = a.n_q_heads, hkv = a.n_kv_heads, D = a.head_dim, half = D / 2;
-  const int heads = hq + 2 * hkv;
-  const int b = blockIdx.x / heads, head = blockIdx.x - b * heads;
-  const uint16_t* src = a.qkv + ((int64_t)b * heads + head) * D;
+  const uint16_t* src = a.qkv + (row * (hq + 2 * hkv) + head) * D;
   const int i = threadIdx.x;
   if (head >= hq + hkv) {                      // a value head: copied
-    uint16_t* dst = a.v + ((int64_t)b * hkv + (head - hq - hkv)) * D;
+    uint16_t* dst = a.v + (row * hkv + (head - hq - hkv)) * D;
     for (int e = i; e < D; e += kWave) dst[e] = src[e];
     return;
   }
   if (i >= half) return;
   const double inv = exp2(-(double)(2 * i) / D * a.log2_theta);
   const double two_pi = 6.283185307179586;
-  double ang = (double)a.pos[b] * inv;
+  double ang = (double)pos * inv;
   ang -= two_pi * rint(ang / two_pi);
   float s, c;
   sincosf((float)ang, &s, &c);
   const float x0 = __uint_as_float((uint32_t)src[i] << 16);
   const float x1 = __uint_as_float((uint32_t)src[i + half] << 16);
-  uint16_t* dst = head < hq ? a.q + ((int64_t)b * hq + head) * D : a.k + ((int64_t)b * hkv + (head - hq)) * D;
+  uint16_t* dst = head < hq ? a.q + (row * hq + head) * D : a.k + (row * hkv + (head - hq)) * D;
   dst[i] = (uint16_t)f32_to_bf16_rne(x0 * c - x1 * s);
   dst[i + half] = (uint16_t)f32_to_bf16_rne(x0 * s + x1 * c);
+}
+
+__global__ void __launch_bounds__(kWave) rope_qkv_kernel(const RopeArgs a) {
+  const int heads = a.shape.n_q_heads + 2 * a.shape.n_kv_heads;
+  const int b = blockIdx.x / heads;
+  rope_head(a.shape, b, blockIdx.x - b * heads, a.pos[b]);
+}
+
+// The same with `width` rows per slot, at positions lens[b] on.
+__global__ void __launch_bounds__(kWave) rope_qkv_at_kernel(const RopeShape a, const int32_t* __restrict__ lens,
+                                                            int32_t width) {
+  const int heads = a.n_q_heads + 2 * a.n_kv_heads;
+  const int row = blockIdx.x / heads, b = row / width;
+  rope_head(a, row, blockIdx.x - row * heads, lens[b] + row - b * width);
 }
 
 // silu(gate) * up of four packed bf16 pairs, rounded to bf16.
