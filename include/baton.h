@@ -715,6 +715,43 @@ baton_status baton_paged_attn(const baton_paged_desc* desc, int32_t layer, const
                               const void* v_new, int32_t width, void* out, float scale, void* ws, size_t ws_bytes,
                               hipStream_t stream);
 
+/*
+ * Drafted tokens against a model's logits (speculative decoding).  For every slot b of
+ * batch: target, device rows of vocab logits, target_ld elements from row to row, row b
+ * width + i following the step's i-th new token (the last accepted one, then the
+ * drafts); drafted, device [batch][width - 1], the tokens drafted for those rows;
+ * n_draft, device [batch] (NULL: width - 1 each): how many of them there are, a
+ * negative number for a free slot; draft: the logits they were drawn from, row b (width
+ * - 1) + i, or NULL if the draft is a token and no distribution (looked up, or the
+ * likeliest).  u_accept [batch][width - 1], u_token [batch]: uniform random numbers.
+ * temperature, top_k, top_p, min_p: device, [batch] each, as baton_sample's.
+ *
+ * With p_i the distribution baton_sample draws from for the slot's i-th row and q_i the
+ * same of the draft's row (all at the drafted token without draft logits), draft x = drafted[i] is
+ * accepted if all in front of it are and u_accept[i] q_i(x) < p_i(x).  At the first one
+ * that is not, a token is drawn from max(0, p_i - q_i), behind the last one from p, as
+ * baton_sample draws: the first in order of index at which the running weight exceeds
+ * u_token times all of it.  The tokens are then distributed as if drawn from p one by
+ * one.  tokens, device [batch][width]: the accepted drafts, the token drawn, -1 behind;
+ * n_out, device [batch]: their number (1 .. width; 0 and all -1 of a free slot) -- the
+ * `keep` of baton_paged_step.
+ * A drafted token outside the vocabulary is not accepted; where nothing of p is above
+ * q, or a row has nothing to draw, the draw is from p; -1 where p has nothing.  Random numbers
+ * are taken into [0, 1), a NaN as 0.  Weights as in baton_sample (p - q in units of
+ * 2^-50): the same inputs give the same tokens.  With width = 1 it is baton_sample.
+ * ws: device workspace, baton_verify_workspace_bytes, 16-byte aligned; calls that share
+ * one go to one stream.
+ * Errors: EINVAL (null or misaligned pointer, batch outside 1 .. BATON_MAX_BATCH, width
+ * outside 1 .. BATON_PAGED_MAX_WIDTH, vocab outside 1 .. 2^24, a row distance below vocab, ws too
+ * small), EDTYPE (not fp32 or bf16), EHIP.
+ */
+size_t baton_verify_workspace_bytes(int32_t batch, int32_t width);
+baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, const void* draft, int64_t draft_ld,
+                          int32_t batch, int32_t width, int32_t vocab, const int32_t* drafted, const int32_t* n_draft,
+                          const float* u_accept, const float* u_token, const float* temperature, const int32_t* top_k,
+                          const float* top_p, const float* min_p, int32_t* tokens, int32_t* n_out, void* ws,
+                          size_t ws_bytes, hipStream_t stream);
+
 /* Static English text of a status. */
 const char* baton_status_string(baton_status status);
 

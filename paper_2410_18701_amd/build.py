@@ -5,7 +5,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libbaton.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("baton.hip", "layer.hip", "adapters.hip", "sample.hip", "paged.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("baton.hip", "layer.hip", "adapters.hip", "sample.hip", "paged.hip", "verify.hip")]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",

@@ -66,6 +66,14 @@ struct SampleArgs {
   int32_t* tokens;
 };
 
+// One row's parameters.
+struct SampleDraw {
+  int32_t vocab, shift;
+  float temperature;
+  int32_t top_k;
+  float top_p, min_p, u;
+};
+
 // Floats (no NaN) as unsigned numbers of the same order, -0 as 0.
 __device__ __forceinline__ uint32_t float_key(float f) {
   const uint32_t b = __float_as_uint(f + 0.f);
@@ -104,6 +112,40 @@ __device__ __forceinline__ uint64_t times_fraction(float f, uint64_t n) {
   const unsigned __int128 x = (unsigned __int128)n * m;
   return (uint64_t)((x + (UP ? ((unsigned __int128)1 << s) - 1 : 0)) >> s);
 }
+
+// exp((x - top) / T) 2^shift with scale = 128 log2(e) / T and table[i] = 2^(i / 128 + shift);
+// least: 128 times the logarithm of a weight that rounds to 0, which a NaN and -inf get.
+__device__ __forceinline__ double sample_weight(const double* table, float x, double top, double scale, double least) {
+  const double y = fmax(((double)x - top) * scale, least);        // 128 log2 w; a NaN is least
+  constexpr double kMagic = 6755399441055744.0;                   // 1.5 * 2^52: rounds to a whole number
+  const double t = y + kMagic;
+  const uint32_t j = (uint32_t)__double_as_longlong(t);
+  const double f = y - (t - kMagic);
+  constexpr double c = 0.0054152123481245727;                     // ln 2 / 128
+  double p = fma(f, c * c * c * c / 24.0, c * c * c / 6.0);
+  p = fma(p, f, c * c / 2.0);
+  p = fma(p, f, c);
+  p = fma(p, f, 1.0);
+  // 2^(j / 128 + shift): the table's entry with j / 128 added to its exponent
+  const double b = __longlong_as_double(__double_as_longlong(table[j & 127]) +
+                                        ((uint64_t)((j & ~127u) << 13) << 32));
+  return p * b;
+}
+// A weight (0 <= wd < 2^52) as a whole number.
+__device__ __forceinline__ uint64_t sample_whole(double wd) {
+  return (uint64_t)__double_as_longlong(wd + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;   // + 2^52
+}
+__device__ __forceinline__ double sample_scale(float temperature) { return 128.0 * 1.4426950408889634074 / (double)temperature; }
+__device__ __forceinline__ double sample_least(int32_t shift) { return -128.0 * (shift + 2); }
+
+// What a row keeps, in place of a token: the weights w (whole numbers) of its tokens x are
+// those of sample_weight with `mx` as the top, of the kept tokens alone: ids (as in
+// the list) from `cut` on, and not below min_p.  one: the first token alone.
+struct SampleKept {
+  uint64_t cut, total;
+  float mx;                      // 1 where the largest is infinite, see SampleRow
+  int32_t infinite, one, none;   // none: no token can be drawn
+};
 
 // Rows of T = fp32 or bf16 (EPV elements per 16 bytes).
 template <typename T>
@@ -193,25 +235,8 @@ struct Sampler {
   }
 
   // The weight of a value, before it is rounded to a whole number (0, of a NaN or -inf).
-  __device__ __forceinline__ double weight(float x) const {
-    const double y = fmax(((double)x - top) * scale, least);        // 128 log2 w; a NaN is least
-    constexpr double kMagic = 6755399441055744.0;                   // 1.5 * 2^52: rounds to a whole number
-    const double t = y + kMagic;
-    const uint32_t j = (uint32_t)__double_as_longlong(t);
-    const double f = y - (t - kMagic);
-    constexpr double c = 0.0054152123481245727;                     // ln 2 / 128
-    double p = fma(f, c * c * c * c / 24.0, c * c * c / 6.0);
-    p = fma(p, f, c * c / 2.0);
-    p = fma(p, f, c);
-    p = fma(p, f, 1.0);
-    // 2^(j / 128 + shift): the table's entry with j / 128 added to its exponent
-    const double b = __longlong_as_double(__double_as_longlong(s.table[j & 127]) +
-                                          ((uint64_t)((j & ~127u) << 13) << 32));
-    return p * b;
-  }
-  __device__ __forceinline__ uint64_t whole(double wd) const {
-    return (uint64_t)__double_as_longlong(wd + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;   // + 2^52
-  }
+  __device__ __forceinline__ double weight(float x) const { return sample_weight(s.table, x, top, scale, least); }
+  __device__ __forceinline__ uint64_t whole(double wd) const { return sample_whole(wd); }
   __device__ __forceinline__ uint32_t valid(float x) const { return x >= mn; }
   __device__ __forceinline__ uint64_t weight_of(float x) const { return whole(weight(x)); }
   // 0 also below min_p (the largest value never is)
@@ -607,14 +632,13 @@ struct Sampler {
   }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs a) {
+// One row: its token, or (KEPT) what it keeps.
+template <typename T, bool KEPT>
+__device__ __forceinline__ void sample_row(SampleShared& s, u32x4* row_lds, const uint8_t* logits, const SampleDraw& a,
+                                           int32_t* token, SampleKept* kept_out) {
   constexpr int EPV = Lane16<T>::kElems;
-  extern __shared__ __attribute__((aligned(16))) u32x4 row_lds[];
-  __shared__ SampleShared s;
-  const int64_t r = blockIdx.x;
   SampleRow<T> row;
-  row.row = a.logits + r * a.ld * T::kBytes;
+  row.row = logits;
   row.off = (int32_t)((reinterpret_cast<uintptr_t>(row.row) & 15u) / T::kBytes);
   row.vocab = a.vocab;
   row.n_vec = (row.off + a.vocab + EPV - 1) / EPV;
@@ -627,12 +651,10 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
   p.v0 = w * p.per;
   p.v1 = min(p.v0 + p.per, row.n_vec);
 
-  const float temperature = a.temperature ? a.temperature[r] : 1.f;
-  const int32_t top_k = a.top_k ? a.top_k[r] : 0;
-  const float top_p = a.top_p ? a.top_p[r] : 1.f;
-  const float min_p = a.min_p ? a.min_p[r] : 0.f;
-  const float u_in = a.u[r];
-  const float u = u_in > 0.f ? fminf(u_in, 0x1.fffffep-1f) : 0.f;       // a NaN is 0
+  const float temperature = a.temperature;
+  const int32_t top_k = a.top_k;
+  const float top_p = a.top_p, min_p = a.min_p;
+  const float u = a.u > 0.f ? fminf(a.u, 0x1.fffffep-1f) : 0.f;       // a NaN is 0
 
   // The row into LDS; its largest value and the smallest that is finite.
   float mx = -INFINITY, mn = INFINITY;
@@ -690,7 +712,10 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
   mx = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(mx)));
   mn = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(mn)));
   if (mx == -INFINITY) {      // no token can be drawn
-    if (tid == 0) a.tokens[r] = -1;
+    if (tid == 0) {
+      if constexpr (KEPT) *kept_out = {0, 0, 0.f, 0, 0, 1};
+      else *token = -1;
+    }
     return;
   }
   p.infinite = mx == INFINITY;             // beside an infinity nothing finite has weight
@@ -705,15 +730,18 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
       atomicMin(&s.index, first);
     }
     __syncthreads();
-    if (tid == 0) a.tokens[r] = (int32_t)s.index;
+    if (tid == 0) {
+      if constexpr (KEPT) *kept_out = {(uint64_t)float_key(mx) << 32 | (uint32_t)~s.index, 1, mx, p.infinite, 1, 0};
+      else *token = (int32_t)s.index;
+    }
     return;
   }
   if (p.infinite) p.own = p.own == INFINITY ? 1.f : -INFINITY;
   p.mx = mx;
   p.mn = mn;
   p.top = (double)mx;
-  p.scale = 128.0 * 1.4426950408889634074 / (double)temperature;
-  p.least = -128.0 * (a.shift + 2);        // a weight that rounds to 0
+  p.scale = sample_scale(temperature);
+  p.least = sample_least(a.shift);
   const bool want_m = min_p > 0.f;
   p.floor_w = want_m ? ldexp((double)min_p, a.shift) : -1.0;
   // Bins over the top of the range: past 32 T below the maximum a weight is under 2^-46.
@@ -723,6 +751,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
   const bool want_k = top_k > 0 && top_k < a.vocab;
   const bool want_p = top_p < 1.f;
   uint64_t cut = 0;       // tokens kept: list ids from here on
+  uint64_t kept_weight = 0;
   uint64_t total;
   if (want_k && top_k <= kSampleTopKList) {
     // A bin up to which at least top_k tokens lie: that of the k-th largest of the
@@ -776,7 +805,22 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
         if (q[e].before_w >= max(need, (uint64_t)1)) g[e] = 0;
         if (want_m && g[e] && !p.weight_if(key_float((uint32_t)(id[e] >> 32)), true)) g[e] = 0;
       }
-      p.draw_list(n, u, id, g, at, a.tokens + r);
+      if constexpr (KEPT) {
+        sum = 0;
+        uint64_t last = ~0ull;         // the last token kept
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          sum += g[e];
+          last = g[e] && id[e] < last ? id[e] : last;
+        }
+        if (tid == 0) s.cut = ~0ull;
+        p.wg_scan(sum, total);
+        atomicMin(reinterpret_cast<unsigned long long*>(&s.cut), (unsigned long long)last);
+        __syncthreads();
+        if (tid == 0) *kept_out = {s.cut, total, mx, p.infinite, 0, 0};
+      } else {
+        p.draw_list(n, u, id, g, at, token);
+      }
       return;
     }
     p.per_bin = weight_bins;
@@ -808,8 +852,8 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
     uint64_t bin_weight = 0;
 #pragma unroll
     for (int q = 0; q < kSampleQuarters; ++q) bin_weight += s.weight[q][tid];
-    uint64_t all_count, kept;
-    const uint64_t to_weight = p.wg_scan(bin_weight, kept);
+    uint64_t all_count;
+    const uint64_t to_weight = p.wg_scan(bin_weight, kept_weight);
     const uint64_t to_count = p.wg_scan(bin_count, all_count);
     // the prefix by count, then the one by weight of what that keeps
 #pragma unroll 1
@@ -817,17 +861,23 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
       uint64_t need = (uint64_t)top_k;
       if (by_weight) {
         if (!want_p) break;
-        need = top_p > 0.f ? max(times_fraction<true>(top_p, kept), (uint64_t)1) : 1;
+        need = top_p > 0.f ? max(times_fraction<true>(top_p, kept_weight), (uint64_t)1) : 1;
       } else if (!want_k || need >= all_count) {
         continue;
       }
       p.select(by_weight != 0, need, by_weight ? bin_weight : bin_count, by_weight ? to_weight : to_count,
                to_weight - bin_weight);
       cut = s.cut;
-      kept = s.before;
+      kept_weight = s.before;
     }
   }
 
+  if constexpr (KEPT) {
+    if (want_p && !want_m) {           // the bins' weights have told
+      if (tid == 0) *kept_out = {cut, kept_weight, mx, p.infinite, 0, 0};
+      return;
+    }
+  }
   const uint32_t cut_key = (uint32_t)(cut >> 32), cut_index = ~(uint32_t)cut;
   const float cut_x = cut ? key_float(cut_key) : mn;
   auto kept = [&](int32_t i, int e, float x) {
@@ -882,7 +932,12 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
           const uint64_t v = p.weight_if(key_float((uint32_t)(id[e] >> 32)), in);
           g[e] = in ? v : 0;
         }
-        p.draw_list(n, u, id, g, at, a.tokens + r);
+        if constexpr (KEPT) {
+          p.wg_scan(g[0] + g[1], total);
+          if (tid == 0) *kept_out = {cut, total, mx, p.infinite, 0, 0};
+        } else {
+          p.draw_list(n, u, id, g, at, token);
+        }
         return;
       }
     }
@@ -899,6 +954,10 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
   __syncthreads();
   total = 0;
   for (int v = 0; v < parts; ++v) total += s.part[v];
+  if constexpr (KEPT) {
+    if (tid == 0) *kept_out = {cut, total, mx, p.infinite, 0, 0};
+    return;
+  }
   // the first token at which the running weight exceeds u * total
   const uint64_t target = times_fraction<false>(u, total);
   uint64_t seen = 0;
@@ -920,13 +979,23 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs
       uint64_t at = upto - mine;
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
-        if (at <= target && at + g[e] > target) a.tokens[r] = (int32_t)row.index(i, e);
+        if (at <= target && at + g[e] > target) *token = (int32_t)row.index(i, e);
         at += g[e];
       }
     }
     seen += all;
     if (seen > target) break;
   }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs a) {
+  extern __shared__ __attribute__((aligned(16))) u32x4 row_lds[];
+  __shared__ SampleShared s;
+  const int64_t r = blockIdx.x;
+  const SampleDraw d = {a.vocab, a.shift, a.temperature ? a.temperature[r] : 1.f, a.top_k ? a.top_k[r] : 0,
+                        a.top_p ? a.top_p[r] : 1.f, a.min_p ? a.min_p[r] : 0.f, a.u[r]};
+  sample_row<T, false>(s, row_lds, a.logits + r * a.ld * T::kBytes, d, a.tokens + r, nullptr);
 }
 
 }  // namespace

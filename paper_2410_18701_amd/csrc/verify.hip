@@ -1,0 +1,85 @@
+// Host side of the verification of drafted tokens: argument checks and launches.  The
+// C ABI is documented in include/baton.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "baton.h"
+#include "verify_kernel.hpp"
+
+namespace {
+
+bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+size_t kept_bytes(int32_t batch, int32_t width) {
+  return ((size_t)batch * (2 * width - 1) * sizeof(baton::SampleKept) + 255) / 256 * 256;
+}
+
+template <typename T>
+baton_status launch(const baton::VerifyArgs& a, hipStream_t s) {
+  const int64_t vec = ((int64_t)a.vocab + 2 * (16 / T::kBytes - 1)) / (16 / T::kBytes);
+  const uint32_t lds = (uint32_t)std::min<int64_t>(vec * 16, baton::kSampleRowBytes);
+  const int32_t rows = a.batch * a.width + (a.draft ? a.batch * (a.width - 1) : 0);
+  hipLaunchKernelGGL(baton::verify_rows_kernel<T>, dim3(rows), dim3(baton::kSampleThreads), lds, s, a);
+  hipLaunchKernelGGL(baton::verify_sums_kernel<T>, dim3(a.segs, a.batch), dim3(baton::kVerifyThreads), 0, s, a);
+  hipLaunchKernelGGL(baton::verify_draw_kernel<T>, dim3(a.batch), dim3(baton::kVerifyThreads), 0, s, a);
+  return hipGetLastError() == hipSuccess ? BATON_OK : BATON_EHIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t baton_verify_workspace_bytes(int32_t batch, int32_t width) {
+  if (batch < 1 || batch > BATON_MAX_BATCH || width < 1 || width > BATON_PAGED_MAX_WIDTH) return 0;
+  return kept_bytes(batch, width) + (size_t)2 * batch * baton::kVerifySegs * sizeof(uint64_t);
+}
+
+baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, const void* draft, int64_t draft_ld,
+                          int32_t batch, int32_t width, int32_t vocab, const int32_t* drafted, const int32_t* n_draft,
+                          const float* u_accept, const float* u_token, const float* temperature, const int32_t* top_k,
+                          const float* top_p, const float* min_p, int32_t* tokens, int32_t* n_out, void* ws,
+                          size_t ws_bytes, hipStream_t stream) {
+  const int64_t most_ld = int64_t(1) << 40;
+  if (batch < 1 || batch > BATON_MAX_BATCH || width < 1 || width > BATON_PAGED_MAX_WIDTH || vocab < 1 ||
+      vocab > (1 << 24) || !target || target_ld < vocab || target_ld > most_ld || !u_token || !tokens || !n_out)
+    return BATON_EINVAL;
+  if (width > 1 && (!drafted || !u_accept || (draft && (draft_ld < vocab || draft_ld > most_ld)))) return BATON_EINVAL;
+  if (dtype != BATON_F32 && dtype != BATON_BF16) return BATON_EDTYPE;
+  const uintptr_t es = dtype == BATON_F32 ? 4 : 2;
+  if (!aligned(target, es) || !aligned(draft, es) || !aligned(drafted, 4) || !aligned(n_draft, 4) ||
+      !aligned(u_accept, 4) || !aligned(u_token, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) ||
+      !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(tokens, 4) || !aligned(n_out, 4))
+    return BATON_EINVAL;
+  if (!ws || !aligned(ws, 16) || ws_bytes < baton_verify_workspace_bytes(batch, width)) return BATON_EINVAL;
+  baton::VerifyArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.target = static_cast<const uint8_t*>(target);
+  a.draft = width > 1 ? static_cast<const uint8_t*>(draft) : nullptr;
+  a.target_ld = target_ld;
+  a.draft_ld = draft_ld;
+  a.batch = batch;
+  a.width = width;
+  a.vocab = vocab;
+  int32_t bits = 0;
+  while ((1 << bits) < vocab) ++bits;
+  a.shift = std::min(62 - bits, 51);
+  a.per_seg = std::max((vocab + baton::kVerifySegs - 1) / baton::kVerifySegs, baton::kVerifyThreads);
+  a.segs = (vocab + a.per_seg - 1) / a.per_seg;
+  a.drafted = drafted;
+  a.n_draft = n_draft;
+  a.u_accept = u_accept;
+  a.u_token = u_token;
+  a.temperature = temperature;
+  a.top_k = top_k;
+  a.top_p = top_p;
+  a.min_p = min_p;
+  a.tokens = tokens;
+  a.n_out = n_out;
+  a.kept = static_cast<baton::SampleKept*>(ws);
+  a.sums = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + kept_bytes(batch, width));
+  return dtype == BATON_F32 ? launch<baton::F32Tag>(a, stream) : launch<baton::BF16Tag>(a, stream);
+}
+
+}  // extern "C"

@@ -203,6 +203,61 @@ class Sampler:
         return self.tokens
 
 
+class Verifier:
+    """Drafted tokens against the target's logits: which are accepted, and the token behind
+    them.  Both results are written to the same tensors by every call: tokens, int32
+    [batch][width], the accepted drafts and the token drawn, -1 behind; n_out, int32 [batch],
+    their number (0 of a free slot), which is PagedCache.begin's keep."""
+
+    def __init__(self, batch, width, vocab):
+        import torch
+        self.batch, self.width, self.vocab = batch, width, vocab
+        self.ws_bytes = B.baton_verify_workspace_bytes(batch, width)
+        if self.ws_bytes == 0:
+            raise ValueError("Verifier: sizes out of range")
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device="cuda")
+        self.tokens = torch.empty((batch, width), dtype=torch.int32, device="cuda")
+        self.n_out = torch.empty(batch, dtype=torch.int32, device="cuda")
+
+    def _rows(self, what, t, n):
+        """The distance of the rows of t [batch][n][vocab], which may be any but the same throughout."""
+        b = self.batch
+        if tuple(t.shape) != (b, n, self.vocab) or (self.vocab > 1 and t.stride(2) != 1) or \
+                (b > 1 and n > 1 and t.stride(0) != n * t.stride(1)):
+            raise ValueError(f"Verifier: {what} must be [batch][{n}][vocab], rows dense and evenly apart")
+        return t.stride(1) if n > 1 else t.stride(0) if b > 1 else self.vocab
+
+    def __call__(self, target, draft, drafted, n_draft, u_accept, u_token, temperature=None, top_k=None, top_p=None,
+                 min_p=None):
+        """target [batch][width][vocab], draft [batch][width - 1][vocab] (or None: the drafts are
+        tokens without a distribution), fp32 or bf16; drafted int32 and u_accept [batch][width - 1];
+        n_draft int32 [batch] (None: all; negative: a free slot); u_token [batch]."""
+        import torch
+        b, w = self.batch, self.width
+        dtype = {torch.float32: B.BATON_F32, torch.bfloat16: B.BATON_BF16}.get(target.dtype)
+        if dtype is None or (draft is not None and draft.dtype != target.dtype):
+            raise ValueError("Verifier: fp32 or bf16 logits, target and draft alike")
+        target_ld = self._rows("target", target, w)
+        if w == 1:
+            draft = drafted = u_accept = None
+        draft_ld = self._rows("draft", draft, w - 1) if draft is not None else 0
+        f32, i32 = torch.float32, torch.int32
+        for name, t, want, n, needed in (
+                ("drafted", drafted, i32, b * (w - 1), w > 1), ("u_accept", u_accept, f32, b * (w - 1), w > 1),
+                ("u_token", u_token, f32, b, True), ("n_draft", n_draft, i32, b, False),
+                ("temperature", temperature, f32, b, False), ("top_k", top_k, i32, b, False),
+                ("top_p", top_p, f32, b, False), ("min_p", min_p, f32, b, False)):
+            if t is None and not needed:
+                continue
+            if t is None or t.dtype != want or t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"Verifier: {name} must be {n} contiguous {want} values")
+        _on_this_gpu("Verifier", self.ws, target, draft, drafted, n_draft, u_accept, u_token, temperature, top_k, top_p,
+                     min_p)
+        B.baton_verify(dtype, target, target_ld, draft, draft_ld, b, w, self.vocab, drafted, n_draft, u_accept, u_token,
+                       temperature, top_k, top_p, min_p, self.tokens, self.n_out, self.ws, self.ws_bytes, _stream())
+        return self.tokens, self.n_out
+
+
 class DecodeLayers:
     """The layers of one model over one BatonCache, with preallocated activations.
 

@@ -1,0 +1,211 @@
+"""Verification of drafted tokens on the GPU against the float64 oracle: whole
+numbers, which have to be equal (random numbers are drawn away from the borders
+by chance: weights have 38 bits or more)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle.verify import kept, verify
+from paper_2410_18701_amd.layer import Sampler, Verifier
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+MODES = {"plain": {}, "temperature": dict(temperature=0.4), "top_k": dict(top_k=20), "top_k_1": dict(top_k=1),
+         "top_k_large": dict(top_k=1500), "top_k_and_p": dict(top_k=60, top_p=0.8), "top_k_large_and_p": dict(top_k=2500, top_p=0.9),
+         "top_p": dict(top_p=0.9), "top_p_low": dict(top_p=0.0), "min_p": dict(min_p=0.1), "min_p_low": dict(min_p=1e-3),
+         "top_p_min_p": dict(top_p=0.95, min_p=0.02), "greedy": dict(temperature=0.0),
+         "all": dict(temperature=0.7, top_k=40, top_p=0.9, min_p=0.05)}
+
+
+def rows(t):
+    return t.double().cpu().numpy()
+
+
+def inputs(seed, batch, width, vocab, dtype, spread=2.5, near=0.7):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    target = spread * torch.randn((batch, width, vocab), generator=g, device="cuda")
+    draft = (target[:, :-1] + near * torch.randn((batch, width - 1, vocab), generator=g, device="cuda")).to(DT[dtype])
+    u = torch.rand((batch, 2 * width), generator=g, device="cuda")
+    return target.to(DT[dtype]), draft, u[:, :width - 1].contiguous(), u[:, width].contiguous(), u[:, width + 1:]
+
+
+def drawn(draft, u, params):
+    """Drafts drawn from the draft's own distribution (by the oracle)."""
+    b, w1, v = draft.shape
+    l, u = rows(draft), u.cpu().numpy()
+    out = np.zeros((b, w1), np.int32)
+    for s in range(b):
+        for i in range(w1):
+            c = np.cumsum(kept(l[s, i], **params[s]))
+            out[s, i] = min(v - 1, int(np.searchsorted(c, u[s, i] * c[-1], side="right"))) if c[-1] > 0 else 0
+    return torch.tensor(out, device="cuda")
+
+
+def tensors(params):
+    get = lambda k, d, t: torch.tensor([p.get(k, d) for p in params], dtype=t, device="cuda")  # noqa: E731
+    return dict(temperature=get("temperature", 1.0, torch.float32), top_k=get("top_k", 0, torch.int32),
+                top_p=get("top_p", 1.0, torch.float32), min_p=get("min_p", 0.0, torch.float32))
+
+
+def f32(params):
+    """The parameters as the library gets them."""
+    return [{k: v if k == "top_k" else float(np.float32(v)) for k, v in p.items()} for p in params]
+
+
+def check(target, draft, drafted, n_draft, ua, ut, params, verifier=None, **given):
+    b, w, v = target.shape
+    tokens, n_out = (verifier or Verifier(b, w, v))(
+        target, draft, drafted, None if n_draft is None else torch.tensor(n_draft, dtype=torch.int32, device="cuda"), ua,
+        ut, **(given or tensors(params)))
+    t, d = rows(target), None if draft is None else rows(draft)
+    x, a, u = drafted.cpu().numpy(), ua.cpu().numpy(), ut.cpu().numpy()
+    accepted = 0
+    for s in range(b):
+        want = verify(t[s], None if d is None else d[s], x[s], w - 1 if n_draft is None else n_draft[s], a[s], float(u[s]),
+                      **f32(params)[s])
+        assert (tokens[s].tolist(), int(n_out[s])) == want, (s, params[s])
+        accepted += want[1] - 1
+    return accepted
+
+
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 3001), ("f32", 2048), ("bf16", 40), ("f32", 1)])
+@pytest.mark.parametrize("mode", MODES)
+def test_against_the_oracle(mode, dtype, vocab):
+    batch, width = 6, 4
+    params = [MODES[mode]] * batch
+    target, draft, ua, ut, ud = inputs(1, batch, width, vocab, dtype)
+    drafted = drawn(draft, ud, f32(params))
+    check(target, draft, drafted, [3, 3, 2, 1, 0, -1], ua, ut, params)
+    check(target, None, drafted, [3, 3, 2, 1, 0, -5], ua, ut, params)
+    check(target, draft, drafted, None, ua, ut, params)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 32000), ("f32", 50257), ("bf16", 128003)])
+def test_large_vocabularies(dtype, vocab):
+    modes = list(MODES.values())
+    params = [modes[i % len(modes)] for i in range(16)]
+    target, draft, ua, ut, ud = inputs(2, 16, 3, vocab, dtype, near=0.3)
+    assert check(target, draft, drawn(draft, ud, f32(params)), None, ua, ut, params) > 5
+
+
+@pytest.mark.parametrize("width", [1, 2, 9, 16])
+def test_widths(width):
+    params = [{}, dict(top_p=0.7), dict(temperature=0.0)]
+    target, draft, ua, ut, ud = inputs(3, 3, width, 1000, "bf16", near=0.2)
+    check(target, draft, drawn(draft, ud[:, :width - 1], f32(params)), None, ua, ut, params)
+
+
+def test_width_one_is_sampling():
+    target, _, _, ut, _ = inputs(4, 32, 1, 5000, "f32")
+    params = [list(MODES.values())[i % len(MODES)] for i in range(32)]
+    tokens, n_out = Verifier(32, 1, 5000)(target, None, None, None, None, ut, **tensors(params))
+    assert torch.equal(tokens[:, 0], Sampler(32, 5000)(target[:, 0], ut, **tensors(params))) and (n_out == 1).all()
+
+
+def test_no_parameters_and_rows_apart():
+    """Rows of a wider buffer that start at odd addresses; no parameters at all."""
+    target, draft, ua, ut, ud = inputs(5, 4, 3, 777, "bf16")
+    params = [{}] * 4
+    drafted = drawn(draft, ud, params)
+    wide = torch.full((12, 801), 50.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, 3:780] = target.flatten(0, 1)
+    v = Verifier(4, 3, 777)
+    check(wide.view(4, 3, 801)[:, :, 3:780], draft, drafted, None, ua, ut, params, verifier=v, temperature=None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_odd_logits(dtype):
+    """-inf, +inf and NaN logits, rows with nothing to draw, in target and draft; drafts out of the vocabulary."""
+    inf, nan = float("inf"), float("nan")
+    batch, width, vocab = 10, 3, 300
+    target, draft, ua, ut, _ = inputs(6, batch, width, vocab, dtype)
+    drafted = torch.randint(0, vocab, (batch, 2), generator=torch.Generator().manual_seed(6)).int().cuda()
+    target[0, 0], target[1, 0, ::2], target[2, 0, 5], target[3, :, 7:] = -inf, nan, inf, -inf
+    target[2, 0, 9], drafted[2, 0] = inf, 9
+    draft[4, 0], draft[5, 0, 3:], draft[6, 0, 100], drafted[6, 0] = nan, -inf, inf, 100
+    target[7], target[8, 0] = nan, 0.0
+    drafted[8, 0], drafted[8, 1], drafted[9, 0] = -1, vocab, 1 << 30
+    drafted[5, 0] = 1
+    for params in ([{}] * batch, [dict(top_p=0.9)] * batch, [dict(top_k=3)] * batch, [dict(temperature=0.0)] * batch):
+        check(target, draft, drafted, None, ua, ut, params)
+        check(target, None, drafted, None, ua, ut, params)
+
+
+def test_the_same_distribution_accepts_everything():
+    target, _, ua, ut, ud = inputs(7, 16, 5, 4000, "bf16")
+    draft = target[:, :-1].contiguous()
+    params = [list(MODES.values())[i % len(MODES)] for i in range(16)]
+    ua[:] = 1.0                                  # taken as the largest number below 1
+    drafted = drawn(draft, ud[:, :4], f32(params))
+    assert check(target, draft, drafted, None, ua, ut, params) == 64
+    ua[:], ut[:] = float("nan"), float("nan")    # as 0
+    check(target, draft, drafted, None, ua, ut, params)
+
+
+def test_equal_logits():
+    """Ties go to the lowest index: prefixes end inside a run of equal logits."""
+    batch, vocab = 6, 6000
+    target = torch.zeros((batch, 2, vocab), dtype=torch.bfloat16, device="cuda")
+    draft = torch.zeros((batch, 1, vocab), dtype=torch.bfloat16, device="cuda")
+    draft[:, :, ::3] = 1.0
+    params = [dict(top_k=2000), dict(top_p=0.5), dict(top_k=50), {}, dict(top_k=3000, top_p=0.5), dict(min_p=0.5)]
+    u = torch.tensor([0.3, 0.9, 0.51, 0.2, 0.7, 0.1], device="cuda")
+    for x in (0, 999, 1998, 2001, 4000):
+        check(target, draft, torch.full((batch, 1), x, dtype=torch.int32, device="cuda"), None, u[:, None].contiguous(), u, params)
+
+
+def test_tokens_are_distributed_as_the_target():
+    """Over 512 x 40 draws the first token's frequencies are p's within five deviations."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    b, vocab, rounds = 512, 24, 40
+    row_t, row_d = torch.randn(2, vocab, generator=g, device="cuda"), torch.randn(vocab, generator=g, device="cuda")
+    target, draft = row_t.expand(b, 2, vocab).contiguous(), row_d.expand(b, 1, vocab).contiguous()
+    par = dict(temperature=0.9, top_p=0.97)
+    q, p = kept(rows(row_d), **f32([par])[0]), kept(rows(row_t[0]), **f32([par])[0])
+    counts, v, params = np.zeros(vocab), Verifier(b, 2, vocab), tensors([par] * b)
+    for _ in range(rounds):
+        x = torch.multinomial(torch.tensor(q, device="cuda"), b, replacement=True, generator=g).int()[:, None]
+        u = torch.rand(2, b, generator=g, device="cuda")
+        tokens, _ = v(target, draft, x, None, u[0][:, None].contiguous(), u[1], **params)
+        counts += np.bincount(tokens[:, 0].cpu().numpy(), minlength=vocab)
+    n = b * rounds
+    assert (np.abs(counts / n - p) <= 5 * np.sqrt(p * (1 - p) / n) + 1e-9).all()
+
+
+def test_captured_and_repeated():
+    params = [dict(top_p=0.9), {}, dict(top_k=30)]
+    target, draft, ua, ut, ud = inputs(9, 3, 4, 9000, "bf16")
+    drafted, par = drawn(draft, ud[:, :3], f32(params)), tensors(params)
+    n_draft = torch.tensor([3, 2, 3], dtype=torch.int32, device="cuda")
+    v, e = Verifier(3, 4, 9000), Verifier(3, 4, 9000)
+    v(target, draft, drafted, n_draft, ua, ut, **par)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        v(target, draft, drafted, n_draft, ua, ut, **par)
+    g = torch.Generator(device="cuda").manual_seed(10)
+    for i in range(8):
+        ua.copy_(torch.rand(ua.shape, generator=g, device="cuda"))
+        ut.copy_(torch.rand(ut.shape, generator=g, device="cuda"))
+        n_draft.copy_(torch.tensor([i % 4, 3, -(i % 2)], dtype=torch.int32))
+        graph.replay()
+        want = e(target, draft, drafted, n_draft, ua, ut, **par)
+        torch.cuda.synchronize()
+        assert torch.equal(v.tokens, want[0]) and torch.equal(v.n_out, want[1])
+
+
+def test_wrapper_refusals():
+    target, draft, ua, ut, _ = inputs(11, 2, 3, 50, "bf16")
+    x = torch.zeros((2, 2), dtype=torch.int32, device="cuda")
+    v = Verifier(2, 3, 50)
+    v(target, draft, x, None, ua, ut)
+    for bad in ((target.half(), draft, x, None, ua, ut), (target, draft.float(), x, None, ua, ut),
+                (target[:, :2], draft, x, None, ua, ut), (target, draft, x.long(), None, ua, ut),
+                (target, draft, None, None, ua, ut), (target, draft, x, None, ua[:, :1], ut), (target, draft, x, x, ua, ut),
+                (target, draft, x, None, ua, None), (target, draft, x, None, ua.cpu(), ut),
+                (target.transpose(0, 1).contiguous().transpose(0, 1), draft, x, None, ua, ut)):
+        with pytest.raises(ValueError):
+            v(*bad)
+    for bad in (dict(batch=0, width=1, vocab=5), dict(batch=1, width=17, vocab=5)):
+        with pytest.raises(ValueError):
+            Verifier(**bad)

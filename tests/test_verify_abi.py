@@ -1,0 +1,79 @@
+"""Host checks of the verification of drafted tokens on the CPU (fake addresses:
+every call returns before any device work), and its oracle against closed
+forms and the distribution it has to give."""
+import numpy as np
+import pytest
+
+from oracle.sampling import sample
+from oracle.verify import kept, verify
+from paper_2410_18701_amd import baton as B
+
+X, Y, Z, W = 0x10000, 0x20000, 0x30000, 0x40000
+
+
+def status(dtype=B.BATON_BF16, target=X, target_ld=100, draft=Y, draft_ld=100, batch=4, width=3, vocab=100, drafted=Z,
+           n_draft=Z, u_accept=Z, u_token=Z, temperature=0, top_k=0, top_p=0, min_p=0, tokens=Z, n_out=Z, ws=W,
+           ws_bytes=1 << 20):
+    try:
+        B.baton_verify(dtype, target, target_ld, draft, draft_ld, batch, width, vocab, drafted, n_draft, u_accept, u_token,
+                       temperature, top_k, top_p, min_p, tokens, n_out, ws, ws_bytes)
+    except B.BatonError as e:
+        return e.status
+    return B.BATON_OK
+
+
+@pytest.mark.parametrize("kw", [
+    dict(target=0), dict(target=X + 1), dict(dtype=B.BATON_F32, target=X + 2), dict(dtype=B.BATON_F32, draft=Y + 2),
+    dict(target_ld=99), dict(draft_ld=99), dict(target_ld=(1 << 40) + 1), dict(batch=0), dict(batch=513), dict(width=0),
+    dict(width=17), dict(vocab=0), dict(vocab=(1 << 24) + 1, target_ld=1 << 25, draft_ld=1 << 25), dict(drafted=0),
+    dict(drafted=Z + 2), dict(n_draft=Z + 1), dict(u_accept=0), dict(u_accept=Z + 2), dict(u_token=0), dict(tokens=0),
+    dict(tokens=Z + 1), dict(n_out=0), dict(n_out=Z + 2), dict(temperature=Z + 1), dict(top_k=Z + 2), dict(top_p=Z + 3),
+    dict(min_p=Z + 1), dict(ws=0), dict(ws=W + 8), dict(ws_bytes=64)], ids=lambda kw: "-".join(kw))
+def test_refusals(kw):
+    assert status(**kw) == B.BATON_EINVAL
+
+
+def test_other_statuses():
+    assert status(dtype=B.BATON_MXFP4) == B.BATON_EDTYPE
+    assert B.baton_verify_workspace_bytes(0, 1) == 0 and B.baton_verify_workspace_bytes(1, 17) == 0
+    assert status(ws_bytes=B.baton_verify_workspace_bytes(4, 3) - 1) == B.BATON_EINVAL
+
+
+def test_oracle_kept_is_what_sampling_draws_from():
+    rng = np.random.default_rng(0)
+    l = rng.normal(size=50)
+    us = (np.arange(4000) + 0.5) / 4000
+    for kw in (dict(), dict(top_k=7), dict(top_p=0.6), dict(min_p=0.3), dict(temperature=0.5, top_k=9, top_p=0.9),
+               dict(temperature=0.0)):
+        drawn = np.bincount([sample(l, u, **kw) for u in us], minlength=50) / 4000
+        assert np.abs(drawn - kept(l, **kw)).max() < 1 / 2000
+
+
+def test_oracle_closed_forms():
+    p, q = np.array([0.1, 0.4, 0.2, 0.3]), np.array([0.4, 0.1, 0.2, 0.3])
+    t, d = np.log(np.array([p, p])), np.log(q[None])
+    assert verify(t, d, [1], 1, [0.99], 0.55) == ([1, 2], 2)          # p > q: always; then from p
+    assert verify(t, d, [0], 1, [0.24], 0.5)[0][0] == 0               # p / q = 1/4
+    assert verify(t, d, [0], 1, [0.26], 0.5) == ([1, -1], 1)          # max(0, p - q) is token 1 alone
+    assert verify(t, None, [3], 1, [0.29], 0.0) == ([3, 0], 2)
+    assert verify(t, None, [3], 1, [0.31], 0.99) == ([2, -1], 1)      # p without token 3
+    assert verify(t, d, [9], 1, [0.0], 0.5) == ([1, -1], 1)           # outside the vocabulary
+    assert verify(t, d, [0], 0, [0.9], 0.05) == ([0, -1], 1)          # no drafts
+    assert verify(t, d, [0], -1, [0.9], 0.05) == ([-1, -1], 0)        # a free slot
+    assert verify(t, t[:1], [2], 1, [0.999], 0.05) == ([2, 0], 2)     # the same distribution
+    # planted: a residual of p itself is another token
+    assert verify(t, d, [0], 1, [0.26], 0.99)[0][0] == 1 and sample(np.log(p), 0.99) == 3
+
+
+def test_oracle_draws_from_the_target():
+    """Over random numbers the first token is distributed as p, whatever the draft's q."""
+    rng = np.random.default_rng(1)
+    t, d = rng.normal(size=(2, 8)), rng.normal(size=(1, 8))
+    kw = dict(temperature=0.8, top_p=0.95)
+    q = kept(d[0], **kw)
+    n = 20000
+    got = np.zeros(8)
+    for x, ua, ut in zip(rng.choice(8, n, p=q), rng.random(n), rng.random(n)):
+        got[verify(t, d, [x], 1, [ua], ut, **kw)[0][0]] += 1
+    p = kept(t[0], **kw)
+    assert (np.abs(got / n - p) <= 5 * np.sqrt(p * (1 - p) / n) + 1e-9).all()
