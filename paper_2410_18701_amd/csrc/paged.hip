@@ -73,7 +73,8 @@ void launch_attn(const baton::PagedAttnArgs& a, int32_t items, bool split, hipSt
   hipLaunchKernelGGL((baton::paged_attn_kernel<T, D, MT>), dim3((unsigned)items * a.n_kv_heads),
                      dim3(baton::kWave * baton::kPagedWaves), 0, s, a);
   if (split)
-    hipLaunchKernelGGL((baton::paged_combine_kernel<T, D>), dim3((unsigned)a.batch * a.n_kv_heads), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((baton::paged_combine_kernel<T, D>), dim3((unsigned)a.batch * a.n_kv_heads, (unsigned)(a.width * a.group)),
+                       dim3(256), 0, s, a);
 }
 
 template <typename T, int D>

@@ -111,8 +111,8 @@ __device__ __forceinline__ void paged_scores(const typename PagedGeo<T, D>::Vecs
   }
 }
 
-// o += V^T P^T over 32 tokens.  EXACT: all of the weights' bits (values that are finite).
-template <typename T, int D, bool EXACT>
+// o += V^T P^T over 32 tokens, finite values.
+template <typename T, int D>
 __device__ __forceinline__ void paged_values(const typename PagedGeo<T, D>::Vecs& vw, const float (&p)[8],
                                              pa_f32x4 (&o)[D / 16]) {
   constexpr int DT = D / 16;
@@ -127,7 +127,7 @@ __device__ __forceinline__ void paged_values(const typename PagedGeo<T, D>::Vecs
     for (int t = 0; t < DT; ++t) {
       const pa_bf16x8 v = __builtin_bit_cast(pa_bf16x8, vw[t]);
       o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, o[t], 0, 0, 0);
-      if constexpr (EXACT) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, o[t], 0, 0, 0);
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, o[t], 0, 0, 0);
     }
   } else {
 #pragma unroll
@@ -137,6 +137,41 @@ __device__ __forceinline__ void paged_values(const typename PagedGeo<T, D>::Vecs
 #pragma unroll
         for (int t = 0; t < DT; ++t)
           o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[tl * DT + t][r]), p[4 * tl + r], o[t], 0, 0, 0);
+  }
+}
+
+// The same for the rows of one new token alone (`mine`), of the tokens of `keep` (bit e:
+// this lane's token 8 (lane / 16) + e): the others' values, which may be infinite or NaN,
+// are left out.  bf16: weights of 8 bits, of which none is 0 beside an infinite value.
+template <typename T, int D>
+__device__ __forceinline__ void paged_values_of(const typename PagedGeo<T, D>::Vecs& vw, const float (&p)[8], uint32_t keep,
+                                                bool mine, pa_f32x4 (&o)[D / 16]) {
+  constexpr int DT = D / 16;
+  if constexpr (T::kBytes == 2) {
+    pa_bf16x8 hi;
+    u32x4 m;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) hi[e] = (__bf16)p[e];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      m[e] = ((keep >> (2 * e)) & 1u ? 0xFFFFu : 0u) | ((keep >> (2 * e + 1)) & 1u ? 0xFFFF0000u : 0u);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const pa_f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pa_bf16x8, vw[t] & m), hi,
+                                                                 pa_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      if (mine) o[t] += x;
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      pa_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t v = (keep >> e) & 1u ? vw[e / 4 * DT + t][e % 4] : 0u;
+        x = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v), p[e], x, 0, 0, 0);
+      }
+      if (mine) o[t] += x;
+    }
   }
 }
 
@@ -183,9 +218,11 @@ template <typename T, int D, int MT>
 __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_kernel(const PagedAttnArgs a) {
   using Geo = PagedGeo<T, D>;
   constexpr int DT = Geo::kDt, CH = Geo::kChunks, NV = Geo::kVecs;
-  // The merge: half of the waves' sums at a time, their rows' maxima and sums.
-  __shared__ __attribute__((aligned(16))) float sm_o[kPagedWaves / 2][MT * DT][kWave][4];
-  __shared__ float sm_m[kPagedWaves][MT * 16], sm_l[kPagedWaves][MT * 16];
+  constexpr bool kQInLds = MT > 1;         // registers hold one tile's queries
+  constexpr int kMerge = kPagedWaves / 2 * MT * DT, kQueries = kQInLds ? MT * CH : 0;
+  // The rows' queries; then the merge: half of the waves' sums at a time.
+  __shared__ u32x4 sm[kMerge > kQueries ? kMerge : kQueries][kWave];
+  __shared__ float sm_m[kPagedWaves][MT * 16], sm_l[kPagedWaves][MT * 16];   // rows' maxima and sums
   const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
   if (item >= a.state[kNumItems]) return;
   const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];
@@ -194,20 +231,56 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_kernel(const P
   const int g4 = lane / 16, c16 = lane % 16;
   const int32_t G = a.group, rows = it.n_new * G;
   const int32_t p_first = it.len, p_last = it.len + it.n_new - 1;
+  const int32_t shift = a.page_shift - 5;                 // blocks per page
+  const int32_t* const table = a.table + (int64_t)it.b * a.max_pages;
+
+  // This wave's blocks: v0 + w, + 4, ...  Their pages, a lane each, 64 at a time.
+  const int32_t n_mine = (it.v1 - it.v0 - w + kPagedWaves - 1) / kPagedWaves;
+  auto block_of = [&](int32_t k) {
+    const int32_t v = it.v0 + w + k * kPagedWaves;
+    return v < it.sink ? v : v + it.skip;
+  };
+  auto pages_from = [&](int32_t k0) {
+    const int32_t page = block_of(k0 + lane) >> shift;
+    const int32_t id = k0 + lane < n_mine && page < a.max_pages ? table[page] : -1;
+    return (uint32_t)id < (uint32_t)a.n_pages ? id : -1;
+  };
+  int32_t ids = pages_from(0);
+  auto offset_of = [&](int32_t id, int32_t block) {
+    return ((((int64_t)id * a.n_kv_heads + h) << shift) + (block & ((1 << shift) - 1))) *
+           (int64_t)(kPagedBlock * Geo::kRow);
+  };
+  if (a.k_new) {       // the new tokens of its blocks (the last ones) first
+    for (int32_t k = n_mine - 1; k >= 0 && block_of(k) * kPagedBlock + kPagedBlock > it.len; --k) {
+      const int32_t block = block_of(k), page = block >> shift;
+      const int32_t id = __builtin_amdgcn_readfirstlane(page < a.max_pages ? table[page] : -1);
+      if ((uint32_t)id >= (uint32_t)a.n_pages) continue;
+      const int64_t off = offset_of(id, block);
+      paged_append<T, D>(a, it, h, block, a.k + off, a.v + off, lane);
+    }
+  }
 
   // The rows: their queries as the second operand, and their positions.
-  u32x4 qw[MT][CH];
+  u32x4 qr[CH];
   int32_t pos[MT];
   const uint8_t* const q = a.q + ((int64_t)it.b * a.width * a.n_kv_heads * G + h * G) * Geo::kRow;
+  auto query = [&](int32_t r, int c) {
+    return r < rows ? *reinterpret_cast<const u32x4*>(q + ((int64_t)(r / G) * a.n_kv_heads * G + r % G) * Geo::kRow +
+                                                      (c * 4 + g4) * 16)
+                    : u32x4{0, 0, 0, 0};
+  };
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const int32_t r = mt * 16 + c16, i = r / G;
-    pos[mt] = r < rows ? it.len + i : -1;
+    const int32_t r = mt * 16 + c16;
+    pos[mt] = r < rows ? it.len + r / G : -1;
+  }
+  if constexpr (kQInLds) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-      qw[mt][c] = r < rows ? *reinterpret_cast<const u32x4*>(q + ((int64_t)i * a.n_kv_heads * G + r % G) * Geo::kRow +
-                                                             (c * 4 + g4) * 16)
-                           : u32x4{0, 0, 0, 0};
+    for (int u = w; u < MT * CH; u += kPagedWaves) sm[u][lane] = query(u / CH * 16 + c16, u % CH);
+    __syncthreads();
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) qr[c] = query(c16, c);
   }
   float m[MT], l[MT];
   pa_f32x4 o[MT][DT];
@@ -219,71 +292,79 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_kernel(const P
     for (int t = 0; t < DT; ++t) o[mt][t] = pa_f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int32_t shift = a.page_shift - 5;                 // blocks per page
-  const int32_t* const table = a.table + (int64_t)it.b * a.max_pages;
-  for (int32_t vb = it.v0 + w; vb < it.v1; vb += kPagedWaves) {
-    const int32_t block = vb < it.sink ? vb : vb + it.skip;
-    const int32_t id = __builtin_amdgcn_readfirstlane((block >> shift) < a.max_pages ? table[block >> shift] : -1);
-    if ((uint32_t)id >= (uint32_t)a.n_pages) continue;    // tokens without a page are not seen
-    const int64_t off = ((((int64_t)id * a.n_kv_heads + h) << shift) + (block & ((1 << shift) - 1))) *
-                        (int64_t)(kPagedBlock * Geo::kRow);
-    const int32_t j0 = block * kPagedBlock;
-    if (a.k_new && j0 + kPagedBlock > it.len) paged_append<T, D>(a, it, h, block, a.k + off, a.v + off, lane);
-    u32x4 kw[NV], vw[NV];
-    const u32x4* const kp = reinterpret_cast<const u32x4*>(a.k + off) + lane;
-    const u32x4* const vp = reinterpret_cast<const u32x4*>(a.v + off) + lane;
+  // K of the next block is asked for when the scores are done, V when it has been used, so
+  // that one of them is always on its way.
+  typename Geo::Vecs kw, vw;
+  auto load = [&](typename Geo::Vecs& x, const uint8_t* from, int32_t k) {
+    const int32_t id = __builtin_amdgcn_readlane(ids, k % kWave);
+    // (a block without a page: the pool's first one, not looked at)
+    const u32x4* const p = reinterpret_cast<const u32x4*>(from + offset_of(max(id, 0), block_of(k))) + lane;
 #pragma unroll
-    for (int u = 0; u < NV; ++u) kw[u] = kp[u * kWave];
+    for (int u = 0; u < NV; ++u) x[u] = __builtin_nontemporal_load(p + u * kWave);
+  };
+  if (n_mine > 0) {
+    load(kw, a.k, 0);
+    load(vw, a.v, 0);
+  }
+  for (int32_t k = 0; k < n_mine; ++k) {
+    const bool there = __builtin_amdgcn_readlane(ids, k % kWave) >= 0;    // tokens without a page are not seen
+    const int32_t j0 = block_of(k) * kPagedBlock;
+    if ((k + 1) % kWave == 0) ids = pages_from(k + 1);
+    const bool more = k + 1 < n_mine;
+    float s[MT][8];
 #pragma unroll
-    for (int u = 0; u < NV; ++u) vw[u] = vp[u * kWave];
+    for (int mt = 0; mt < MT; ++mt) {
+      if (mt > 0 && mt * 16 >= rows) break;
+      if constexpr (kQInLds) {
+        u32x4 qw[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) qw[c] = sm[mt * CH + c][lane];
+        paged_scores<T, D>(kw, qw, s[mt]);
+      } else {
+        paged_scores<T, D>(kw, qr, s[mt]);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) load(kw, a.k, k + 1);
+    __builtin_amdgcn_sched_barrier(0);
 
     // All rows see all of the block, but where it holds new tokens or the window's start.
-    const bool whole = j0 + kPagedBlock - 1 <= p_first &&
+    const bool whole = there && j0 + kPagedBlock - 1 <= p_first &&
                        (a.window == 0 || j0 > p_last - a.window || j0 + kPagedBlock <= a.sinks);
     const int32_t jl = j0 + 8 * g4;                       // this lane's first token
-    // Bit e: position p sees token jl + e.
-    auto sees = [&](int32_t p) {
+    // Bit e: a token at a position from p0 to p1 sees token jl + e.
+    auto sees = [&](int32_t p0, int32_t p1) {
       uint32_t bits = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int32_t j = jl + e;
-        bits |= j <= p && (a.window == 0 || j > p - a.window || j < a.sinks) ? 1u << e : 0u;
+        bits |= there && j <= p1 && (a.window == 0 || j > p0 - a.window || j < a.sinks) ? 1u << e : 0u;
       }
       return bits;
     };
-    if (!whole) {      // tokens that no row sees: anything may lie there
-      uint32_t any = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int32_t j = jl + e;
-        any |= j <= p_last && (a.window == 0 || j > p_first - a.window || j < a.sinks) ? 1u << e : 0u;
-      }
-      paged_clear<T, D>(vw, any);
-    }
+    if (!whole) paged_clear<T, D>(vw, sees(p_first, p_last));   // what no row sees: anything may lie there
     const bool odd = paged_odd<T, D>(vw);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      if (mt * 16 >= rows) break;
-      float s[8], p[8];
-      paged_scores<T, D>(kw, qw[mt], s);
+      if (mt > 0 && mt * 16 >= rows) break;
       if (whole) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] *= a.qscale;
+        for (int e = 0; e < 8; ++e) s[mt][e] *= a.qscale;
       } else {
-        const uint32_t bits = sees(pos[mt]);
+        const uint32_t bits = sees(pos[mt], pos[mt]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = (bits >> e) & 1u ? s[e] * a.qscale : -INFINITY;
+        for (int e = 0; e < 8; ++e) s[mt][e] = (bits >> e) & 1u ? s[mt][e] * a.qscale : -INFINITY;
       }
-      float mx = s[0];
+      float mx = s[mt][0], p[8];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
+      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[mt][e]);
       const float mn = fmaxf(m[mt], max_over_groups(mx));
       const float ref = mn == -INFINITY ? 0.f : mn;       // nothing seen yet
       const float alpha = fast_exp2(m[mt] - ref);
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        p[e] = fast_exp2(s[e] - ref);
+        p[e] = fast_exp2(s[mt][e] - ref);
         sum += p[e];
       }
       m[mt] = mn;
@@ -291,24 +372,15 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_kernel(const P
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[mt][t] *= alpha;
       if (!odd) {
-        paged_values<T, D, true>(vw, p, o[mt]);
-        continue;
-      }
-      for (int32_t i = mt * 16 / G; i < it.n_new && i * G < mt * 16 + 16; ++i) {
-        u32x4 vi[NV];
-#pragma unroll
-        for (int u = 0; u < NV; ++u) vi[u] = vw[u];
-        paged_clear<T, D>(vi, sees(it.len + i));
-        pa_f32x4 oi[DT];
-#pragma unroll
-        for (int t = 0; t < DT; ++t) oi[t] = pa_f32x4{0.f, 0.f, 0.f, 0.f};
-        paged_values<T, D, false>(vi, p, oi);
-        if (pos[mt] == it.len + i) {
-#pragma unroll
-          for (int t = 0; t < DT; ++t) o[mt][t] += oi[t];
-        }
+        paged_values<T, D>(vw, p, o[mt]);
+      } else {
+        for (int32_t i = mt * 16 / G; i < it.n_new && i * G < mt * 16 + 16; ++i)
+          paged_values_of<T, D>(vw, p, sees(it.len + i, it.len + i), pos[mt] == it.len + i, o[mt]);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) load(vw, a.v, k + 1);
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   // The waves' sums, each relative to its row's maximum in the wave, brought to the
@@ -321,7 +393,7 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_kernel(const P
       sm_l[w][mt * 16 + c16] = l[mt];
     }
   }
-  __syncthreads();
+  __syncthreads();                         // (and the queries have been read)
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float mx = sm_m[0][mt * 16 + c16], sum = 0.f;
@@ -342,14 +414,14 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_kernel(const P
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int t = 0; t < DT; ++t) *reinterpret_cast<pa_f32x4*>(sm_o[w - half][mt * DT + t][lane]) = o[mt][t];
+        for (int t = 0; t < DT; ++t) sm[((w - half) * MT + mt) * DT + t][lane] = __builtin_bit_cast(u32x4, o[mt][t]);
     }
     __syncthreads();
     if (w < half) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int t = 0; t < DT; ++t) o[mt][t] += *reinterpret_cast<const pa_f32x4*>(sm_o[w][mt * DT + t][lane]);
+        for (int t = 0; t < DT; ++t) o[mt][t] += __builtin_bit_cast(pa_f32x4, sm[(w * MT + mt) * DT + t][lane]);
     }
     __syncthreads();
   }
@@ -385,39 +457,55 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_kernel(const P
   }
 }
 
-// Rows of slots with several work items: their partial sums, in order.  One workgroup per
-// (slot, head), D / 4 threads per row.
+// Rows of slots with several work items: their partial sums.  One workgroup per (slot,
+// head) and row; D / 4 threads hold the columns, the others' groups take every
+// 256 / (D / 4)-th item, and their sums are added in order.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnArgs a) {
   using Geo = PagedGeo<T, D>;
-  const int32_t b = blockIdx.x / a.n_kv_heads, h = blockIdx.x - b * a.n_kv_heads;
+  constexpr int TC = D / 4, NG = 256 / TC;
+  __shared__ float sm_m[4], sm_l[NG];
+  __shared__ __attribute__((aligned(16))) float sm_o[NG][D];
+  const int32_t b = blockIdx.x / a.n_kv_heads, h = blockIdx.x - b * a.n_kv_heads, r = blockIdx.y;
   const int32_t first = a.state[a.at.first + b], parts = a.state[a.at.first + b + 1] - first;
   const int32_t n_new = a.state[a.at.n_new + b];
-  if (parts < 2 || n_new > a.width) return;
-  const int32_t G = a.group, rows = n_new * G, max_rows = a.width * G;
-  const int32_t d4 = threadIdx.x % (D / 4);
+  const int32_t G = a.group, max_rows = a.width * G;
+  if (parts < 2 || n_new > a.width || r >= n_new * G) return;
   const int64_t step = (int64_t)a.n_kv_heads * max_rows * Geo::kRec;
-  for (int32_t r = threadIdx.x / (D / 4); r < rows; r += 256 / (D / 4)) {
-    const float* const rec = a.partial + (((int64_t)first * a.n_kv_heads + h) * max_rows + r) * Geo::kRec;
-    float mx = -INFINITY;
-    for (int32_t s = 0; s < parts; ++s) mx = fmaxf(mx, rec[s * step + D]);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    float sum = 0.f;
-    pa_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const float* const rec = a.partial + (((int64_t)first * a.n_kv_heads + h) * max_rows + r) * Geo::kRec;
+  float mx = -INFINITY;
+  for (int32_t s = threadIdx.x; s < parts; s += 256) mx = fmaxf(mx, rec[s * step + D]);
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, kWave));
+  if (threadIdx.x % kWave == 0) sm_m[threadIdx.x / kWave] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  const int32_t d4 = threadIdx.x % TC, g = threadIdx.x / TC;
+  float sum = 0.f;
+  pa_f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int32_t s = 0; s < parts; ++s) {
-      const float f = fast_exp2(rec[s * step + D] - ref);
-      sum += rec[s * step + D + 1] * f;
-      o += *reinterpret_cast<const pa_f32x4*>(rec + s * step + 4 * d4) * f;
-    }
-    const pa_f32x4 x = o * (sum == 0.f ? 0.f : 1.f / sum);
-    uint8_t* const row = a.out + ((((int64_t)b * a.width + r / G) * a.n_kv_heads + h) * G + r % G) * Geo::kRow;
-    if constexpr (T::kBytes == 2)
-      *reinterpret_cast<uint2*>(row + 8 * d4) = make_uint2(f32_to_bf16_rne(x[0]) | f32_to_bf16_rne(x[1]) << 16,
-                                                          f32_to_bf16_rne(x[2]) | f32_to_bf16_rne(x[3]) << 16);
-    else
-      *reinterpret_cast<pa_f32x4*>(row + 16 * d4) = x;
+  for (int32_t s = g; s < parts; s += NG) {
+    const float f = fast_exp2(rec[s * step + D] - ref);
+    sum += rec[s * step + D + 1] * f;
+    o += *reinterpret_cast<const pa_f32x4*>(rec + s * step + 4 * d4) * f;
   }
+  *reinterpret_cast<pa_f32x4*>(sm_o[g] + 4 * d4) = o;
+  if (d4 == 0) sm_l[g] = sum;
+  __syncthreads();
+  if (g != 0) return;
+#pragma unroll
+  for (int v = 1; v < NG; ++v) {
+    o += *reinterpret_cast<const pa_f32x4*>(sm_o[v] + 4 * d4);
+    sum += sm_l[v];
+  }
+  const pa_f32x4 x = o * (sum == 0.f ? 0.f : 1.f / sum);
+  uint8_t* const row = a.out + ((((int64_t)b * a.width + r / G) * a.n_kv_heads + h) * G + r % G) * Geo::kRow;
+  if constexpr (T::kBytes == 2)
+    *reinterpret_cast<uint2*>(row + 8 * d4) = make_uint2(f32_to_bf16_rne(x[0]) | f32_to_bf16_rne(x[1]) << 16,
+                                                        f32_to_bf16_rne(x[2]) | f32_to_bf16_rne(x[3]) << 16);
+  else
+    *reinterpret_cast<pa_f32x4*>(row + 16 * d4) = x;
 }
 
 }  // namespace baton
