@@ -68,21 +68,14 @@ baton_status check(const baton_paged_desc* d) {
   return BATON_OK;
 }
 
-template <typename T, int D, int MT>
-void launch_attn(const baton::PagedAttnArgs& a, int32_t items, bool split, hipStream_t s) {
-  hipLaunchKernelGGL((baton::paged_attn_kernel<T, D, MT>), dim3((unsigned)items * a.n_kv_heads),
-                     dim3(baton::kWave * baton::kPagedWaves), 0, s, a);
-  if (split)
-    hipLaunchKernelGGL((baton::paged_combine_kernel<T, D>), dim3((unsigned)a.batch * a.n_kv_heads, (unsigned)(a.width * a.group)),
-                       dim3(256), 0, s, a);
-}
-
 template <typename T, int D>
-void launch_attn_rows(const baton::PagedAttnArgs& a, int32_t items, bool split, hipStream_t s) {
-  const int32_t rows = a.width * a.group;
-  if (rows <= 16) launch_attn<T, D, 1>(a, items, split, s);
-  else if (rows <= 32) launch_attn<T, D, 2>(a, items, split, s);
-  else launch_attn<T, D, 4>(a, items, split, s);
+void launch_attn(const baton::PagedAttnArgs& a, int32_t items, bool split, hipStream_t s) {
+  const dim3 grid((unsigned)items * a.n_kv_heads), block(baton::kWave * baton::kPagedWaves);
+  if (a.width * a.group <= 16) hipLaunchKernelGGL((baton::paged_attn_kernel<T, D>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((baton::paged_attn_rows_kernel<T, D>), grid, block, 0, s, a);
+  if (split)
+    hipLaunchKernelGGL((baton::paged_combine_kernel<T, D>),
+                       dim3((unsigned)a.batch * a.n_kv_heads, (unsigned)(a.width * a.group)), dim3(256), 0, s, a);
 }
 
 template <int ES, int D>
@@ -188,9 +181,9 @@ baton_status baton_paged_step(const baton_paged_desc* d, const int32_t* keep, co
   a.window = d->window;
   a.sinks = d->sinks;
   a.n_kv_heads = d->n_kv_heads;
+  a.group = d->n_q_heads / d->n_kv_heads;
   a.width = width;
   a.map_ld = map_ld;
-  a.max_items = max_items(*d);
   a.at = state_at(*d);
   hipLaunchKernelGGL(baton::paged_step_kernel, dim3(1), dim3(baton::kStepThreads), 0, stream, a);
   return done();
@@ -269,11 +262,11 @@ baton_status baton_paged_attn(const baton_paged_desc* d, int32_t layer, const vo
   a.sinks = d->sinks;
   const bool split = need > 0;
   if (d->dtype == BATON_F32) {
-    if (d->head_dim == 64) launch_attn_rows<baton::F32Tag, 64>(a, items, split, stream);
-    else launch_attn_rows<baton::F32Tag, 128>(a, items, split, stream);
+    if (d->head_dim == 64) launch_attn<baton::F32Tag, 64>(a, items, split, stream);
+    else launch_attn<baton::F32Tag, 128>(a, items, split, stream);
   } else {
-    if (d->head_dim == 64) launch_attn_rows<baton::BF16Tag, 64>(a, items, split, stream);
-    else launch_attn_rows<baton::BF16Tag, 128>(a, items, split, stream);
+    if (d->head_dim == 64) launch_attn<baton::BF16Tag, 64>(a, items, split, stream);
+    else launch_attn<baton::BF16Tag, 128>(a, items, split, stream);
   }
   return done();
 }

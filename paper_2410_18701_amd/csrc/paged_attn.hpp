@@ -7,8 +7,7 @@
 // S sinks, j > p - W or j < S.
 //
 // A work item is a run of blocks of 32 tokens of one slot; a workgroup of four waves
-// takes an item for one kv-head, wave w every fourth of its blocks.  Per block, with the
-// matrix cores' 16x16 tiles:
+// takes an item for one kv-head.  Per block and tile, with the matrix cores' 16x16 tiles:
 //  * scores, transposed: S^T = K Q^T, K's rows being the tokens.  Lane l has row l % 16's
 //    scores of the tokens 8 (l / 16) .. + 7.
 //  * softmax with a running maximum per row, in fp32, base 2.
@@ -17,7 +16,7 @@
 // bf16: weights are taken as a sum of two bf16 numbers, so that they have 16 bits for
 // their product with the values; the values' and keys' products are exact in fp32.
 // fp32: products in fp32 (v_mfma_f32_16x16x4_f32).
-// K and V come from memory in the order of the operands, without a trip through LDS.
+// K and V come from memory in the order of the operands.
 // Values that are infinite or NaN: a weight of 0 would turn them into NaN for rows that
 // do not see them.  Blocks that hold any are multiplied once for each new token, with
 // what it does not see set to zero, and added to that token's rows alone.
@@ -199,262 +198,408 @@ __device__ __forceinline__ void paged_clear(typename PagedGeo<T, D>::Vecs& vw, u
   }
 }
 
-// Whether any lane holds a value that is infinite or NaN.
+// Whether any lane holds a value that is infinite or NaN: one that is, by its bits, among
+// the largest as a signed number (positive) or as an unsigned one (negative).
 template <typename T, int D>
 __device__ __forceinline__ bool paged_odd(const typename PagedGeo<T, D>::Vecs& vw) {
-  uint32_t any = 0;
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  if constexpr (T::kBytes == 2) {
+    s16x2 pos = {0, 0};
+    u16x2 neg = {0, 0};
 #pragma unroll
-  for (int u = 0; u < PagedGeo<T, D>::kVecs; ++u)
+    for (int u = 0; u < PagedGeo<T, D>::kVecs; ++u)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      // an exponent of all ones carries into the bit above it
-      if constexpr (T::kBytes == 2) any |= (vw[u][e] & 0x7F807F80u) + 0x00800080u;
-      else any |= (vw[u][e] & 0x7F800000u) + 0x00800000u;
-    }
-  return __any((any & (T::kBytes == 2 ? 0x80008000u : 0x80000000u)) != 0);
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = vw[u][e];
+        pos = __builtin_elementwise_max(pos, __builtin_bit_cast(s16x2, x));
+        neg = __builtin_elementwise_max(neg, __builtin_bit_cast(u16x2, x));
+      }
+    return __any(max(pos.x, pos.y) >= 0x7F80 || max(neg.x, neg.y) >= 0xFF80);
+  } else {
+    int32_t pos = 0;
+    uint32_t neg = 0;
+#pragma unroll
+    for (int u = 0; u < PagedGeo<T, D>::kVecs; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        pos = max(pos, (int32_t)vw[u][e]);
+        neg = max(neg, vw[u][e]);
+      }
+    return __any(pos >= 0x7F800000 || neg >= 0xFF800000u);
+  }
 }
 
-template <typename T, int D, int MT>
-__global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_kernel(const PagedAttnArgs a) {
+// What a workgroup's waves know of their item.
+struct PagedRows {
+  int32_t len, n_new, group, window, sinks, shift;   // shift: log2 of a page's blocks
+  float qscale;
+
+  // Bit e: a token at a position from p0 to p1 sees token j + e.
+  __device__ __forceinline__ uint32_t sees(int32_t j, int32_t p0, int32_t p1) const {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bits |= j + e <= p1 && (window == 0 || j + e > p0 - window || j + e < sinks) ? 1u << e : 0u;
+    return bits;
+  }
+  // All rows see all of the block from token j0 on.
+  __device__ __forceinline__ bool whole(int32_t j0) const {
+    return j0 + kPagedBlock - 1 <= len && (window == 0 || j0 > len + n_new - 1 - window || j0 + kPagedBlock <= sinks);
+  }
+};
+
+// A tile of 16 rows: lane l has row l % 16, its running maximum, its sum over the lane's
+// tokens, and columns 16 t + 4 (l / 16) .. + 3 of its weighted values.
+template <int D>
+struct PagedTile {
+  int32_t first, pos;        // the tile's first row; this lane's row's position (-1: no row)
+  float m, l;
+  pa_f32x4 o[D / 16];
+
+  __device__ __forceinline__ PagedTile(const PagedRows& r, int32_t tile, int c16) {
+    first = tile * 16;
+    pos = first + c16 < r.n_new * r.group ? r.len + (first + c16) / r.group : -1;
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) o[t] = pa_f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // One block, from its scores and values.  there: it has a page.
+  template <typename T>
+  __device__ __forceinline__ void add(const PagedRows& r, int32_t j0, bool there, float (&s)[8],
+                                      typename PagedGeo<T, D>::Vecs& vw, int g4) {
+    const bool whole = there && r.whole(j0);
+    const int32_t jl = j0 + 8 * g4;
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] *= r.qscale;
+    } else {
+      const uint32_t bits = there ? r.sees(jl, pos, pos) : 0u;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] = (bits >> e) & 1u ? s[e] * r.qscale : -INFINITY;
+      // what no row sees: anything may lie there
+      paged_clear<T, D>(vw, there ? r.sees(jl, r.len, r.len + r.n_new - 1) : 0u);
+    }
+    float mx = s[0], p[8];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
+    const float mn = fmaxf(m, max_over_groups(mx));
+    const float ref = mn == -INFINITY ? 0.f : mn;       // nothing seen yet
+    const float alpha = fast_exp2(m - ref);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = fast_exp2(s[e] - ref);
+      sum += p[e];
+    }
+    m = mn;
+    l = l * alpha + sum;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
+    if (!paged_odd<T, D>(vw)) {
+      paged_values<T, D>(vw, p, o);
+    } else {
+      for (int32_t i = first / r.group; i < r.n_new && i * r.group < first + 16; ++i)
+        paged_values_of<T, D>(vw, p, there ? r.sees(jl, r.len + i, r.len + i) : 0u, pos == r.len + i, o);
+    }
+  }
+};
+
+// The row's result, or its partial record if the slot has several items.
+template <typename T, int D>
+__device__ __forceinline__ void paged_write(const PagedAttnArgs& a, const PagedItem& it, int32_t item, int32_t h,
+                                            const PagedTile<D>& x, int lane) {
   using Geo = PagedGeo<T, D>;
-  constexpr int DT = Geo::kDt, CH = Geo::kChunks, NV = Geo::kVecs;
-  constexpr bool kQInLds = MT > 1;         // registers hold one tile's queries
-  constexpr int kMerge = kPagedWaves / 2 * MT * DT, kQueries = kQInLds ? MT * CH : 0;
-  // The rows' queries; then the merge: half of the waves' sums at a time.
-  __shared__ u32x4 sm[kMerge > kQueries ? kMerge : kQueries][kWave];
-  __shared__ float sm_m[kPagedWaves][MT * 16], sm_l[kPagedWaves][MT * 16];   // rows' maxima and sums
+  const int g4 = lane / 16, c16 = lane % 16;
+  const int32_t parts = a.state[a.at.first + it.b + 1] - a.state[a.at.first + it.b];
+  const int32_t G = a.group, r = x.first + c16;
+  if (r >= it.n_new * G) return;
+  if (parts == 1) {
+    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
+    uint8_t* const row = a.out + ((((int64_t)it.b * a.width + r / G) * a.n_kv_heads + h) * G + r % G) * Geo::kRow;
+#pragma unroll
+    for (int t = 0; t < Geo::kDt; ++t) {
+      const pa_f32x4 y = x.o[t] * inv;
+      if constexpr (T::kBytes == 2)
+        *reinterpret_cast<uint2*>(row + (16 * t + 4 * g4) * 2) =
+            make_uint2(f32_to_bf16_rne(y[0]) | f32_to_bf16_rne(y[1]) << 16,
+                       f32_to_bf16_rne(y[2]) | f32_to_bf16_rne(y[3]) << 16);
+      else
+        *reinterpret_cast<pa_f32x4*>(row + (16 * t + 4 * g4) * 4) = y;
+    }
+  } else {
+    float* const rec = a.partial + (((int64_t)item * a.n_kv_heads + h) * (a.width * G) + r) * Geo::kRec;
+#pragma unroll
+    for (int t = 0; t < Geo::kDt; ++t) *reinterpret_cast<pa_f32x4*>(rec + 16 * t + 4 * g4) = x.o[t];
+    if (g4 == 0) {
+      rec[D] = x.m;
+      rec[D + 1] = x.l;
+    }
+  }
+}
+
+// Waves that have the same tile (`groups` of them, a power of two; wave w is of group
+// w / (4 / groups)) bring their sums together: in the first group's.  Each sum is
+// relative to its own maximum; half of the groups at a time hand theirs over in LDS.
+template <int D>
+__device__ __forceinline__ void paged_merge(PagedTile<D>& x, int32_t groups, u32x4 (*sm)[kWave],
+                                            float (*sm_m)[16], float (*sm_l)[16], int w, int lane) {
+  constexpr int DT = D / 16;
+  const int g4 = lane / 16, c16 = lane % 16;
+  const int tiles = kPagedWaves / groups, tile = w % tiles, group = w / tiles;
+  x.l = sum_over_groups(x.l);
+  if (g4 == 0) {
+    sm_m[w][c16] = x.m;
+    sm_l[w][c16] = x.l;
+  }
+  __syncthreads();
+  float mx = -INFINITY, sum = 0.f;
+  for (int v = tile; v < kPagedWaves; v += tiles) mx = fmaxf(mx, sm_m[v][c16]);
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  for (int v = tile; v < kPagedWaves; v += tiles) sum += sm_l[v][c16] * fast_exp2(sm_m[v][c16] - ref);
+  const float f = fast_exp2(x.m - ref);
+#pragma unroll
+  for (int t = 0; t < DT; ++t) x.o[t] *= f;
+  x.m = mx;
+  x.l = sum;
+  for (int half = groups / 2; half > 0; half /= 2) {
+    u32x4(*const at)[kWave] = sm + (((group % half) * tiles) + tile) * DT;
+    if (group >= half && group < 2 * half) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t) at[t][lane] = __builtin_bit_cast(u32x4, x.o[t]);
+    }
+    __syncthreads();
+    if (group < half) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t) x.o[t] += __builtin_bit_cast(pa_f32x4, at[t][lane]);
+    }
+    __syncthreads();
+  }
+}
+
+// The page of block `block` of the item's slot, -1 if it has none.
+__device__ __forceinline__ int32_t paged_page(const PagedAttnArgs& a, const PagedItem& it, int32_t block, int32_t shift) {
+  const int32_t page = block >> shift;
+  const int32_t id = page < a.max_pages ? a.table[(int64_t)it.b * a.max_pages + page] : -1;
+  return (uint32_t)id < (uint32_t)a.n_pages ? id : -1;
+}
+template <typename T, int D>
+__device__ __forceinline__ int64_t paged_offset(const PagedAttnArgs& a, int32_t id, int32_t h, int32_t block, int32_t shift) {
+  return ((((int64_t)id * a.n_kv_heads + h) << shift) + (block & ((1 << shift) - 1))) *
+         (int64_t)(kPagedBlock * PagedGeo<T, D>::kRow);
+}
+// The item's k-th block.
+__device__ __forceinline__ int32_t paged_block_of(const PagedItem& it, int32_t k) {
+  const int32_t v = it.v0 + k;
+  return v < it.sink ? v : v + it.skip;
+}
+// 16 bytes of row r's query.
+template <typename T, int D>
+__device__ __forceinline__ u32x4 paged_query(const PagedAttnArgs& a, const PagedItem& it, int32_t h, int32_t r, int c, int g4) {
+  const int32_t G = a.group;
+  if (r >= it.n_new * G) return u32x4{0, 0, 0, 0};
+  const int64_t row = (((int64_t)it.b * a.width + r / G) * a.n_kv_heads + h) * G + r % G;
+  return *reinterpret_cast<const u32x4*>(a.q + row * PagedGeo<T, D>::kRow + (c * 4 + g4) * 16);
+}
+
+// All of the wave's loads are done.  They are, where this stands, but for the branch that
+// lanes without a block take; told so, the compiler does not wait in the loops behind it.
+__device__ __forceinline__ void paged_wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+// Up to 16 rows.  Every wave has all of them, and every fourth of the item's blocks, whose
+// keys and values go from memory into its registers.
+template <typename T, int D>
+__global__ void __launch_bounds__(kWave * kPagedWaves) __attribute__((amdgpu_waves_per_eu(T::kBytes == 4 && D == 128 ? 1 : 2)))
+paged_attn_kernel(const PagedAttnArgs a) {
+  using Geo = PagedGeo<T, D>;
+  constexpr int CH = Geo::kChunks, NV = Geo::kVecs;
+  __shared__ u32x4 sm[kPagedWaves / 2 * Geo::kDt][kWave];
+  __shared__ float sm_m[kPagedWaves][16], sm_l[kPagedWaves][16];
   const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
   if (item >= a.state[kNumItems]) return;
   const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];
   if (it.n_new > a.width) return;          // a prompt: it comes whole, with its attention done
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int g4 = lane / 16, c16 = lane % 16;
-  const int32_t G = a.group, rows = it.n_new * G;
-  const int32_t p_first = it.len, p_last = it.len + it.n_new - 1;
-  const int32_t shift = a.page_shift - 5;                 // blocks per page
-  const int32_t* const table = a.table + (int64_t)it.b * a.max_pages;
+  const PagedRows r = {it.len, it.n_new, a.group, a.window, a.sinks, a.page_shift - 5, a.qscale};
 
-  // This wave's blocks: v0 + w, + 4, ...  Their pages, a lane each, 64 at a time.
+  // This wave's blocks: w, w + 4, ... of the item.
   const int32_t n_mine = (it.v1 - it.v0 - w + kPagedWaves - 1) / kPagedWaves;
-  auto block_of = [&](int32_t k) {
-    const int32_t v = it.v0 + w + k * kPagedWaves;
-    return v < it.sink ? v : v + it.skip;
-  };
-  auto pages_from = [&](int32_t k0) {
-    const int32_t page = block_of(k0 + lane) >> shift;
-    const int32_t id = k0 + lane < n_mine && page < a.max_pages ? table[page] : -1;
-    return (uint32_t)id < (uint32_t)a.n_pages ? id : -1;
-  };
-  int32_t ids = pages_from(0);
-  auto offset_of = [&](int32_t id, int32_t block) {
-    return ((((int64_t)id * a.n_kv_heads + h) << shift) + (block & ((1 << shift) - 1))) *
-           (int64_t)(kPagedBlock * Geo::kRow);
-  };
+  auto block_of = [&](int32_t k) { return paged_block_of(it, w + k * kPagedWaves); };
   if (a.k_new) {       // the new tokens of its blocks (the last ones) first
     for (int32_t k = n_mine - 1; k >= 0 && block_of(k) * kPagedBlock + kPagedBlock > it.len; --k) {
-      const int32_t block = block_of(k), page = block >> shift;
-      const int32_t id = __builtin_amdgcn_readfirstlane(page < a.max_pages ? table[page] : -1);
-      if ((uint32_t)id >= (uint32_t)a.n_pages) continue;
-      const int64_t off = offset_of(id, block);
+      const int32_t block = block_of(k), id = __builtin_amdgcn_readfirstlane(paged_page(a, it, block, r.shift));
+      if (id < 0) continue;
+      const int64_t off = paged_offset<T, D>(a, id, h, block, r.shift);
       paged_append<T, D>(a, it, h, block, a.k + off, a.v + off, lane);
     }
   }
+  u32x4 qw[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) qw[c] = paged_query<T, D>(a, it, h, c16, c, g4);
+  PagedTile<D> x(r, 0, c16);
 
-  // The rows: their queries as the second operand, and their positions.
-  u32x4 qr[CH];
-  int32_t pos[MT];
-  const uint8_t* const q = a.q + ((int64_t)it.b * a.width * a.n_kv_heads * G + h * G) * Geo::kRow;
-  auto query = [&](int32_t r, int c) {
-    return r < rows ? *reinterpret_cast<const u32x4*>(q + ((int64_t)(r / G) * a.n_kv_heads * G + r % G) * Geo::kRow +
-                                                      (c * 4 + g4) * 16)
-                    : u32x4{0, 0, 0, 0};
-  };
+  // 64 blocks at a time, whose pages are in a lane each.  K of the next block is asked for
+  // when the scores are done, V when it has been used, so that one of them is always on its way.
+  for (int32_t k0 = 0; k0 < n_mine; k0 += kWave) {
+    const int32_t n = min(n_mine - k0, kWave);
+    const int32_t ids = lane < n ? paged_page(a, it, block_of(k0 + lane), r.shift) : -1;
+    paged_wait_loads();
+    typename Geo::Vecs kw, vw;
+    auto load = [&](typename Geo::Vecs& to, const uint8_t* from, int32_t k) {
+      const int32_t id = __builtin_amdgcn_readlane(ids, k);
+      // (a block without a page: the pool's first one, not looked at)
+      const u32x4* const p =
+          reinterpret_cast<const u32x4*>(from + paged_offset<T, D>(a, max(id, 0), h, block_of(k0 + k), r.shift)) + lane;
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int32_t r = mt * 16 + c16;
-    pos[mt] = r < rows ? it.len + r / G : -1;
-  }
-  if constexpr (kQInLds) {
-#pragma unroll
-    for (int u = w; u < MT * CH; u += kPagedWaves) sm[u][lane] = query(u / CH * 16 + c16, u % CH);
-    __syncthreads();
-  } else {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) qr[c] = query(c16, c);
-  }
-  float m[MT], l[MT];
-  pa_f32x4 o[MT][DT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    m[mt] = -INFINITY;
-    l[mt] = 0.f;
-#pragma unroll
-    for (int t = 0; t < DT; ++t) o[mt][t] = pa_f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  // K of the next block is asked for when the scores are done, V when it has been used, so
-  // that one of them is always on its way.
-  typename Geo::Vecs kw, vw;
-  auto load = [&](typename Geo::Vecs& x, const uint8_t* from, int32_t k) {
-    const int32_t id = __builtin_amdgcn_readlane(ids, k % kWave);
-    // (a block without a page: the pool's first one, not looked at)
-    const u32x4* const p = reinterpret_cast<const u32x4*>(from + offset_of(max(id, 0), block_of(k))) + lane;
-#pragma unroll
-    for (int u = 0; u < NV; ++u) x[u] = __builtin_nontemporal_load(p + u * kWave);
-  };
-  if (n_mine > 0) {
+      for (int u = 0; u < NV; ++u) to[u] = __builtin_nontemporal_load(p + u * kWave);
+    };
     load(kw, a.k, 0);
     load(vw, a.v, 0);
-  }
-  for (int32_t k = 0; k < n_mine; ++k) {
-    const bool there = __builtin_amdgcn_readlane(ids, k % kWave) >= 0;    // tokens without a page are not seen
-    const int32_t j0 = block_of(k) * kPagedBlock;
-    if ((k + 1) % kWave == 0) ids = pages_from(k + 1);
-    const bool more = k + 1 < n_mine;
-    float s[MT][8];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      if (mt > 0 && mt * 16 >= rows) break;
-      if constexpr (kQInLds) {
-        u32x4 qw[CH];
-#pragma unroll
-        for (int c = 0; c < CH; ++c) qw[c] = sm[mt * CH + c][lane];
-        paged_scores<T, D>(kw, qw, s[mt]);
-      } else {
-        paged_scores<T, D>(kw, qr, s[mt]);
-      }
+    for (int32_t k = 0; k < n; ++k) {
+      const bool there = __builtin_amdgcn_readlane(ids, k) >= 0;    // tokens without a page are not seen
+      const bool more = k + 1 < n;
+      float s[8];
+      paged_scores<T, D>(kw, qw, s);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) load(kw, a.k, k + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      x.template add<T>(r, block_of(k0 + k) * kPagedBlock, there, s, vw, g4);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) load(vw, a.v, k + 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (more) load(kw, a.k, k + 1);
-    __builtin_amdgcn_sched_barrier(0);
+  }
+  paged_merge<D>(x, kPagedWaves, sm, sm_m, sm_l, w, lane);
+  if (w == 0) paged_write<T, D>(a, it, item, h, x, lane);
+}
 
-    // All rows see all of the block, but where it holds new tokens or the window's start.
-    const bool whole = there && j0 + kPagedBlock - 1 <= p_first &&
-                       (a.window == 0 || j0 > p_last - a.window || j0 + kPagedBlock <= a.sinks);
-    const int32_t jl = j0 + 8 * g4;                       // this lane's first token
-    // Bit e: a token at a position from p0 to p1 sees token jl + e.
-    auto sees = [&](int32_t p0, int32_t p1) {
-      uint32_t bits = 0;
+// This wave's LDS reads and all but its last VM vector loads are done, then the barrier:
+// __syncthreads() does not promise that another wave's loads into LDS have landed.
+template <int VM>
+__device__ __forceinline__ void paged_wait_and_barrier() {
+  static_assert(VM < 16, "vmcnt's low four bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | VM);       // vmcnt <= VM, lgkmcnt 0
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// 1 KB from `from` into LDS at `to`, lane l's 16 bytes (l16 = 16 l) at 16 l.  In asm: the
+// compiler would wait for such loads before reads of other buffers (it keeps only a few of
+// them apart).  They have no result in registers, and are waited for at the barriers.
+__device__ __forceinline__ void paged_load_lds(const uint8_t* from, uint32_t l16, u32x4* to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to), "v"(l16), "s"(from)
+               : "memory", "m0");
+#endif
+}
+
+// Up to 64 rows.  Blocks go from memory into LDS, without registers, some blocks ahead, and
+// the waves share them: with more than 32 rows each wave has a tile of its own, with 32 two
+// waves share a tile and take turns at the blocks, with 16 all four do.
+template <typename T, int D>
+__global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_rows_kernel(const PagedAttnArgs a) {
+  using Geo = PagedGeo<T, D>;
+  constexpr int CH = Geo::kChunks, NV = Geo::kVecs;
+  constexpr int BB = 2 * NV * 1024;              // bytes of a block's K and V
+  constexpr int R = BB <= 16384 ? 4 : 3;         // blocks in LDS
+  constexpr int NL = 2 * NV / kPagedWaves;       // loads per wave and block
+  // a buffer each, not an array: reads of one must not wait for the loads into another
+  __shared__ __attribute__((aligned(1024))) u32x4 buf0[2 * NV][kWave], buf1[2 * NV][kWave], buf2[2 * NV][kWave];
+  __shared__ __attribute__((aligned(1024))) u32x4 buf3[R == 4 ? 2 * NV : 1][kWave];
+  __shared__ float sm_m[kPagedWaves][16], sm_l[kPagedWaves][16];
+  const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
+  if (item >= a.state[kNumItems]) return;
+  const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];
+  if (it.n_new > a.width) return;          // a prompt: it comes whole, with its attention done
+  const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int g4 = lane / 16, c16 = lane % 16;
+  const PagedRows r = {it.len, it.n_new, a.group, a.window, a.sinks, a.page_shift - 5, a.qscale};
+  const int32_t n = it.v1 - it.v0, rows = it.n_new * a.group;
+  const int32_t tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, groups = kPagedWaves / tiles;
+  const int32_t tile = w % tiles, turn = w / tiles;
+
+  if (a.k_new) {       // the new tokens of the item's blocks (the last ones) first, a wave a block
+    for (int32_t k = n - 1; k >= 0 && paged_block_of(it, k) * kPagedBlock + kPagedBlock > it.len; --k) {
+      const int32_t block = paged_block_of(it, k), id = __builtin_amdgcn_readfirstlane(paged_page(a, it, block, r.shift));
+      if (id < 0 || k % kPagedWaves != w) continue;
+      const int64_t off = paged_offset<T, D>(a, id, h, block, r.shift);
+      paged_append<T, D>(a, it, h, block, a.k + off, a.v + off, lane);
+    }
+    __syncthreads();
+  }
+  u32x4 qw[CH];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int32_t j = jl + e;
-        bits |= there && j <= p1 && (a.window == 0 || j > p0 - a.window || j < a.sinks) ? 1u << e : 0u;
+  for (int c = 0; c < CH; ++c) qw[c] = paged_query<T, D>(a, it, h, tile * 16 + c16, c, g4);
+  PagedTile<D> x(r, tile, c16);
+
+  // 64 blocks at a time, whose pages are in a lane each.
+  for (int32_t k0 = 0; k0 < n; k0 += kWave) {
+    const int32_t nk = min(n - k0, kWave);
+    const int32_t ids = lane < nk ? paged_page(a, it, paged_block_of(it, k0 + lane), r.shift) : -1;
+    paged_wait_loads();
+    int32_t fetched = 0;
+    // The next block into LDS, a fourth of it by this wave (past the last one: that one
+    // again, so that the number of loads on their way is always the same).
+    auto fetch = [&](u32x4 (*to)[kWave]) {
+      const int32_t k = min(fetched, nk - 1), id = __builtin_amdgcn_readlane(ids, k);
+      const int64_t off = paged_offset<T, D>(a, max(id, 0), h, paged_block_of(it, k0 + k), r.shift);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {       // chunks of K, then of V
+        const int c = (i < NL / 2 ? i : i - NL / 2) * kPagedWaves + w;
+        paged_load_lds((i < NL / 2 ? a.k : a.v) + off + c * 1024, lane * 16, to[(i < NL / 2 ? 0 : NV) + c]);
       }
-      return bits;
+      ++fetched;
     };
-    if (!whole) paged_clear<T, D>(vw, sees(p_first, p_last));   // what no row sees: anything may lie there
-    const bool odd = paged_odd<T, D>(vw);
+    // Block k from its buffer.  The barrier comes after every load but those of the R - 2
+    // blocks behind it, and after every wave's reads of block k - 1, whose buffer is free then.
+    auto step = [&](int32_t k, u32x4 (*from)[kWave], u32x4 (*free)[kWave]) {
+      paged_wait_and_barrier<NL * (R - 2)>();
+      fetch(free);
+      if ((k0 + k) % groups != turn || tile * 16 >= rows) return;
+      float s[8];
+      {
+        typename Geo::Vecs kw;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      if (mt > 0 && mt * 16 >= rows) break;
-      if (whole) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[mt][e] *= a.qscale;
-      } else {
-        const uint32_t bits = sees(pos[mt], pos[mt]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[mt][e] = (bits >> e) & 1u ? s[mt][e] * a.qscale : -INFINITY;
+        for (int u = 0; u < NV; ++u) kw[u] = from[u][lane];
+        paged_scores<T, D>(kw, qw, s);
       }
-      float mx = s[mt][0], p[8];
+      typename Geo::Vecs vw;
 #pragma unroll
-      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[mt][e]);
-      const float mn = fmaxf(m[mt], max_over_groups(mx));
-      const float ref = mn == -INFINITY ? 0.f : mn;       // nothing seen yet
-      const float alpha = fast_exp2(m[mt] - ref);
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = fast_exp2(s[mt][e] - ref);
-        sum += p[e];
-      }
-      m[mt] = mn;
-      l[mt] = l[mt] * alpha + sum;
-#pragma unroll
-      for (int t = 0; t < DT; ++t) o[mt][t] *= alpha;
-      if (!odd) {
-        paged_values<T, D>(vw, p, o[mt]);
-      } else {
-        for (int32_t i = mt * 16 / G; i < it.n_new && i * G < mt * 16 + 16; ++i)
-          paged_values_of<T, D>(vw, p, sees(it.len + i, it.len + i), pos[mt] == it.len + i, o[mt]);
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (more) load(vw, a.v, k + 1);
-    __builtin_amdgcn_sched_barrier(0);
-  }
-
-  // The waves' sums, each relative to its row's maximum in the wave, brought to the
-  // largest of the four: two waves hand theirs to the other two, then one to the first.
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    l[mt] = sum_over_groups(l[mt]);
-    if (g4 == 0) {
-      sm_m[w][mt * 16 + c16] = m[mt];
-      sm_l[w][mt * 16 + c16] = l[mt];
-    }
-  }
-  __syncthreads();                         // (and the queries have been read)
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    float mx = sm_m[0][mt * 16 + c16], sum = 0.f;
-#pragma unroll
-    for (int v = 1; v < kPagedWaves; ++v) mx = fmaxf(mx, sm_m[v][mt * 16 + c16]);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-#pragma unroll
-    for (int v = 0; v < kPagedWaves; ++v) sum += sm_l[v][mt * 16 + c16] * fast_exp2(sm_m[v][mt * 16 + c16] - ref);
-    const float f = fast_exp2(m[mt] - ref);
-#pragma unroll
-    for (int t = 0; t < DT; ++t) o[mt][t] *= f;
-    m[mt] = mx;
-    l[mt] = sum;
-  }
-#pragma unroll
-  for (int half = kPagedWaves / 2; half > 0; half /= 2) {
-    if (w >= half && w < 2 * half) {
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int t = 0; t < DT; ++t) sm[((w - half) * MT + mt) * DT + t][lane] = __builtin_bit_cast(u32x4, o[mt][t]);
-    }
-    __syncthreads();
-    if (w < half) {
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int t = 0; t < DT; ++t) o[mt][t] += __builtin_bit_cast(pa_f32x4, sm[(w * MT + mt) * DT + t][lane]);
-    }
-    __syncthreads();
-  }
-  if (w != 0) return;
-  const int32_t parts = a.state[a.at.first + it.b + 1] - a.state[a.at.first + it.b];
-  const int32_t max_rows = a.width * G;
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int32_t r = mt * 16 + c16;
-    if (r >= rows) continue;
-    if (parts == 1) {
-      const float inv = l[mt] == 0.f ? 0.f : 1.f / l[mt];
-      uint8_t* const row = a.out + ((((int64_t)it.b * a.width + r / G) * a.n_kv_heads + h) * G + r % G) * Geo::kRow;
-#pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const pa_f32x4 x = o[mt][t] * inv;
-        if constexpr (T::kBytes == 2)
-          *reinterpret_cast<uint2*>(row + (16 * t + 4 * g4) * 2) =
-              make_uint2(f32_to_bf16_rne(x[0]) | f32_to_bf16_rne(x[1]) << 16,
-                         f32_to_bf16_rne(x[2]) | f32_to_bf16_rne(x[3]) << 16);
-        else
-          *reinterpret_cast<pa_f32x4*>(row + (16 * t + 4 * g4) * 4) = x;
+      for (int u = 0; u < NV; ++u) vw[u] = from[NV + u][lane];
+      x.template add<T>(r, paged_block_of(it, k0 + k) * kPagedBlock, __builtin_amdgcn_readlane(ids, k) >= 0, s, vw, g4);
+    };
+    fetch(buf0);
+    fetch(buf1);
+    if constexpr (R == 4) {
+      fetch(buf2);
+      for (int32_t k = 0;; k += 4) {
+        step(k, buf0, buf3);
+        if (k + 1 >= nk) break;
+        step(k + 1, buf1, buf0);
+        if (k + 2 >= nk) break;
+        step(k + 2, buf2, buf1);
+        if (k + 3 >= nk) break;
+        step(k + 3, buf3, buf2);
+        if (k + 4 >= nk) break;
       }
     } else {
-      float* const rec = a.partial + (((int64_t)item * a.n_kv_heads + h) * max_rows + r) * Geo::kRec;
-#pragma unroll
-      for (int t = 0; t < DT; ++t) *reinterpret_cast<pa_f32x4*>(rec + 16 * t + 4 * g4) = o[mt][t];
-      if (g4 == 0) {
-        rec[D] = m[mt];
-        rec[D + 1] = l[mt];
+      for (int32_t k = 0;; k += 3) {
+        step(k, buf0, buf2);
+        if (k + 1 >= nk) break;
+        step(k + 1, buf1, buf0);
+        if (k + 2 >= nk) break;
+        step(k + 2, buf2, buf1);
+        if (k + 3 >= nk) break;
       }
     }
+    paged_wait_and_barrier<0>();                    // no load is on its way into what is used next
   }
+  paged_merge<D>(x, groups, buf0, sm_m, sm_l, w, lane);
+  if (turn == 0) paged_write<T, D>(a, it, item, h, x, lane);
 }
 
 // Rows of slots with several work items: their partial sums.  One workgroup per (slot,

@@ -18,7 +18,9 @@
 namespace baton {
 
 constexpr int kPagedBlock = 32;          // tokens per block
-constexpr int kPagedItems = 2048;        // work items of an attention launch, about
+constexpr int kPagedMaxNew = 16;         // == BATON_PAGED_MAX_WIDTH
+constexpr int kPagedItems = 2048;        // workgroups of an attention launch, about
+constexpr int kPagedRowItems = 512;      // and with more than 16 rows per head, which two a compute unit fill
 constexpr int kPagedMinBlocks = 8;       // blocks per work item, at least
 
 // A slot's work item: visible blocks v0 .. v1 - 1 of slot b, the `part`-th of `parts`.
@@ -61,7 +63,7 @@ struct PagedStepArgs {
   const int32_t* n_new;
   int32_t* slot_map;        // null: not wanted
   int32_t* missing;         // null: not wanted
-  int32_t batch, max_pages, page_shift, window, sinks, n_kv_heads, width, map_ld, max_items;
+  int32_t batch, max_pages, page_shift, window, sinks, n_kv_heads, group, width, map_ld;
   PagedState at;
 };
 
@@ -170,7 +172,7 @@ __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedSte
   }
   // Visible blocks of 32 tokens, and work items.
   int32_t blocks = 0, sink = 0, skip = 0;
-  if (slot && now > 0) {
+  if (slot && now > 0 && now <= kPagedMaxNew) {       // (a prompt comes with its attention done)
     const int32_t end = (len + now + kPagedBlock - 1) / kPagedBlock;
     const int32_t from = a.window > 0 ? max(0, len - a.window + 1) / kPagedBlock : 0;
     sink = min((min(a.sinks, len + now) + kPagedBlock - 1) / kPagedBlock, from);
@@ -182,10 +184,15 @@ __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedSte
   s_sink[b] = sink;
   s_skip[b] = skip;
   s_blocks[b] = blocks;
-  int32_t n_blocks, n_items;
+  // Items of `per` blocks, so that there are about as many as the launch has workgroups: a
+  // live slot's last one is half full.
+  int32_t n_blocks, n_live, n_items;
   step_scan(blocks, sums, n_blocks);
-  const int32_t target = kPagedItems / a.n_kv_heads + 1;
-  const int32_t per = max(kPagedMinBlocks, (n_blocks + target - 1) / target);
+  step_scan(blocks > 0, sums, n_live);
+  const bool many = __syncthreads_or(blocks > 0 && now * a.group > 16);
+  const int32_t target = (many ? kPagedRowItems : kPagedItems) / a.n_kv_heads;
+  const int32_t whole = max(target - n_live / 2, target / 4 + 1);
+  const int32_t per = max(kPagedMinBlocks, (n_blocks + whole - 1) / whole);
   const int32_t items = (blocks + per - 1) / per;
   first_item[b] = step_scan(items, sums, n_items);
   if (b == 0) first_item[kStepThreads] = n_items;
