@@ -745,7 +745,7 @@ baton_status baton_paged_attn(const baton_paged_desc* desc, int32_t layer, const
  * outside 1 .. BATON_PAGED_MAX_WIDTH, vocab outside 1 .. 2^24, a row distance below vocab, ws too
  * small), EDTYPE (not fp32 or bf16), EHIP.
  */
-size_t baton_verify_workspace_bytes(int32_t batch, int32_t width);
+size_t baton_verify_workspace_bytes(int32_t batch, int32_t width, int32_t vocab);
 baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, const void* draft, int64_t draft_ld,
                           int32_t batch, int32_t width, int32_t vocab, const int32_t* drafted, const int32_t* n_draft,
                           const float* u_accept, const float* u_token, const float* temperature, const int32_t* top_k,

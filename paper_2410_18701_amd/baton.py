@@ -117,7 +117,7 @@ def lib():
         L.baton_paged_attn_workspace_bytes.argtypes = [pd, i32]
         L.baton_paged_attn_workspace_bytes.restype = sz
         L.baton_paged_attn.argtypes = [pd, i32, vp, vp, vp, i32, vp, ctypes.c_float, vp, sz, vp]
-        L.baton_verify_workspace_bytes.argtypes = [i32, i32]
+        L.baton_verify_workspace_bytes.argtypes = [i32, i32, i32]
         L.baton_verify_workspace_bytes.restype = sz
         L.baton_verify.argtypes = [i32, vp, i64, vp, i64, i32, i32, i32] + [vp] * 11 + [sz, vp]
         L.baton_status_string.argtypes = [st]
@@ -385,8 +385,8 @@ def baton_paged_attn(desc, layer, q, k_new, v_new, width, out, scale, ws, ws_byt
                                   float(scale), _ptr(ws), ws_bytes, _stream(stream)), "baton_paged_attn")
 
 
-def baton_verify_workspace_bytes(batch, width):
-    return lib().baton_verify_workspace_bytes(batch, width)
+def baton_verify_workspace_bytes(batch, width, vocab):
+    return lib().baton_verify_workspace_bytes(batch, width, vocab)
 
 
 def baton_verify(dtype, target, target_ld, draft, draft_ld, batch, width, vocab, drafted, n_draft, u_accept, u_token,

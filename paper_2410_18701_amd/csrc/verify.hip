@@ -16,12 +16,23 @@ size_t kept_bytes(int32_t batch, int32_t width) {
   return ((size_t)batch * (2 * width - 1) * sizeof(baton::SampleKept) + 255) / 256 * 256;
 }
 
+size_t sums_bytes(int32_t batch) { return (size_t)2 * batch * baton::kVerifyParts * sizeof(uint64_t); }
+
+// Pieces of a row of `bytes`-byte elements, at the worst alignment of its first one.
+int32_t row_pieces(int32_t vocab, int32_t bytes) {
+  const int32_t per = 16 / bytes, vecs = (int32_t)(((int64_t)vocab + 2 * (per - 1)) / per);
+  const int32_t each = baton::kVerifyThreads * baton::kVerifyVecs;
+  return (vecs + each - 1) / each;
+}
+
 template <typename T>
 baton_status launch(const baton::VerifyArgs& a, hipStream_t s) {
   const int64_t vec = ((int64_t)a.vocab + 2 * (16 / T::kBytes - 1)) / (16 / T::kBytes);
-  const uint32_t lds = (uint32_t)std::min<int64_t>(vec * 16, baton::kSampleRowBytes);
-  const int32_t rows = a.batch * a.width + (a.draft ? a.batch * (a.width - 1) : 0);
-  hipLaunchKernelGGL(baton::verify_rows_kernel<T>, dim3(rows), dim3(baton::kSampleThreads), lds, s, a);
+  int64_t lds = (sizeof(baton::SampleShared) + 15) / 16 * 16 + std::min<int64_t>(vec * 16, baton::kSampleRowBytes);
+  if (T::kBytes == 2) lds = std::max<int64_t>(lds, sizeof(baton::ValueShared));
+  const int32_t rows = a.batch * a.slot_rows;
+  hipLaunchKernelGGL(baton::verify_pieces_kernel<T>, dim3(a.n_pieces, rows), dim3(baton::kVerifyThreads), 0, s, a);
+  hipLaunchKernelGGL(baton::verify_rows_kernel<T>, dim3(rows), dim3(baton::kSampleThreads), (uint32_t)lds, s, a);
   hipLaunchKernelGGL(baton::verify_sums_kernel<T>, dim3(a.segs, a.batch), dim3(baton::kVerifyThreads), 0, s, a);
   hipLaunchKernelGGL(baton::verify_draw_kernel<T>, dim3(a.batch), dim3(baton::kVerifyThreads), 0, s, a);
   return hipGetLastError() == hipSuccess ? BATON_OK : BATON_EHIP;
@@ -31,9 +42,12 @@ baton_status launch(const baton::VerifyArgs& a, hipStream_t s) {
 
 extern "C" {
 
-size_t baton_verify_workspace_bytes(int32_t batch, int32_t width) {
-  if (batch < 1 || batch > BATON_MAX_BATCH || width < 1 || width > BATON_PAGED_MAX_WIDTH) return 0;
-  return kept_bytes(batch, width) + (size_t)2 * batch * baton::kVerifySegs * sizeof(uint64_t);
+size_t baton_verify_workspace_bytes(int32_t batch, int32_t width, int32_t vocab) {
+  if (batch < 1 || batch > BATON_MAX_BATCH || width < 1 || width > BATON_PAGED_MAX_WIDTH || vocab < 1 ||
+      vocab > (1 << 24))
+    return 0;
+  return kept_bytes(batch, width) + sums_bytes(batch) +
+         (size_t)batch * (2 * width - 1) * row_pieces(vocab, 4) * sizeof(baton::VerifyPiece);
 }
 
 baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, const void* draft, int64_t draft_ld,
@@ -52,7 +66,7 @@ baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, 
       !aligned(u_accept, 4) || !aligned(u_token, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) ||
       !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(tokens, 4) || !aligned(n_out, 4))
     return BATON_EINVAL;
-  if (!ws || !aligned(ws, 16) || ws_bytes < baton_verify_workspace_bytes(batch, width)) return BATON_EINVAL;
+  if (!ws || !aligned(ws, 16) || ws_bytes < baton_verify_workspace_bytes(batch, width, vocab)) return BATON_EINVAL;
   baton::VerifyArgs a;
   std::memset(&a, 0, sizeof(a));
   a.target = static_cast<const uint8_t*>(target);
@@ -65,8 +79,10 @@ baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, 
   int32_t bits = 0;
   while ((1 << bits) < vocab) ++bits;
   a.shift = std::min(62 - bits, 51);
-  a.per_seg = std::max((vocab + baton::kVerifySegs - 1) / baton::kVerifySegs, baton::kVerifyThreads);
-  a.segs = (vocab + a.per_seg - 1) / a.per_seg;
+  // as many segments as fill the GPU: before the first token a workgroup waits for a chain of loads
+  const int32_t parts = std::min(baton::kVerifySegs, std::max(1, 1024 / batch)) * baton::kVerifyWaves;
+  a.per_part = std::max((vocab + parts - 1) / parts, baton::kWave);
+  a.segs = (vocab + baton::kVerifyWaves * a.per_part - 1) / (baton::kVerifyWaves * a.per_part);
   a.drafted = drafted;
   a.n_draft = n_draft;
   a.u_accept = u_accept;
@@ -79,6 +95,9 @@ baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, 
   a.n_out = n_out;
   a.kept = static_cast<baton::SampleKept*>(ws);
   a.sums = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + kept_bytes(batch, width));
+  a.pieces = reinterpret_cast<baton::VerifyPiece*>(reinterpret_cast<char*>(a.sums) + sums_bytes(batch));
+  a.n_pieces = row_pieces(vocab, (int32_t)es);
+  a.slot_rows = a.draft ? 2 * width - 1 : width;
   return dtype == BATON_F32 ? launch<baton::F32Tag>(a, stream) : launch<baton::BF16Tag>(a, stream);
 }
 

@@ -212,7 +212,7 @@ class Verifier:
     def __init__(self, batch, width, vocab):
         import torch
         self.batch, self.width, self.vocab = batch, width, vocab
-        self.ws_bytes = B.baton_verify_workspace_bytes(batch, width)
+        self.ws_bytes = B.baton_verify_workspace_bytes(batch, width, vocab)
         if self.ws_bytes == 0:
             raise ValueError("Verifier: sizes out of range")
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device="cuda")

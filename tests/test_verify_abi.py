@@ -35,8 +35,9 @@ def test_refusals(kw):
 
 def test_other_statuses():
     assert status(dtype=B.BATON_MXFP4) == B.BATON_EDTYPE
-    assert B.baton_verify_workspace_bytes(0, 1) == 0 and B.baton_verify_workspace_bytes(1, 17) == 0
-    assert status(ws_bytes=B.baton_verify_workspace_bytes(4, 3) - 1) == B.BATON_EINVAL
+    assert B.baton_verify_workspace_bytes(0, 1, 5) == 0 and B.baton_verify_workspace_bytes(1, 17, 5) == 0
+    assert B.baton_verify_workspace_bytes(1, 1, 0) == 0 and B.baton_verify_workspace_bytes(1, 1, (1 << 24) + 1) == 0
+    assert status(ws_bytes=B.baton_verify_workspace_bytes(4, 3, 100) - 1) == B.BATON_EINVAL
 
 
 def test_oracle_kept_is_what_sampling_draws_from():
