@@ -462,6 +462,7 @@ struct VerifyRow {
   const uint8_t* row;
   SampleKept kept;
   double top, scale, least, floor;
+  float low;                   // the last kept token's value
 
   __device__ __forceinline__ float value(int32_t i) const {
     if constexpr (T::kBytes == 4) return reinterpret_cast<const float*>(row)[i];
@@ -469,7 +470,7 @@ struct VerifyRow {
   }
   __device__ __forceinline__ uint64_t weight(const double* table, float x, uint32_t index) const {
     if (kept.infinite) x = x == INFINITY ? 1.f : __uint_as_float(0x7FC00000u);
-    if (!(x <= kept.mx) || kept.none) return 0;                       // a NaN
+    if (!(x >= low)) return 0;                                        // below the last kept value, or a NaN
     if (((uint64_t)float_key(x) << 32 | (uint32_t)~index) < kept.cut) return 0;
     if (kept.one) return 1;
     const double d = sample_weight(table, x, top, scale, least);
@@ -484,6 +485,7 @@ __device__ __forceinline__ VerifyRow<T> verify_row(const VerifyArgs& a, const ui
   r.row = rows + at * ld * T::kBytes;
   r.kept = kept[at];
   r.top = (double)r.kept.mx;
+  r.low = r.kept.none ? INFINITY : r.kept.cut ? key_float((uint32_t)(r.kept.cut >> 32)) : -INFINITY;
   r.scale = sample_scale(a.temperature ? a.temperature[b] : 1.f);
   r.least = sample_least(a.shift);
   const float min_p = a.min_p ? a.min_p[b] : 0.f;
@@ -509,17 +511,19 @@ struct VerifyEnd {
     const double d = (double)own * cp - (double)h * cq;
     return d > 0.0 ? sample_whole(d) : 0;
   }
-  // The logits of N tokens from `base` on, `step` apart, below `end` (the others' are -inf).
-  template <int N>
-  __device__ __forceinline__ void values(int64_t base, int32_t step, int64_t end, float (&xp)[N], float (&xq)[N]) const {
+  // The logits of N tokens from `i` on, `step` apart; ALL: below `end` (the others' are -inf).
+  template <int N, bool ALL>
+  __device__ __forceinline__ void values(int32_t i, int32_t step, int32_t end, float (&xp)[N], float (&xq)[N]) const {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const int32_t i = (int32_t)(base + e * step < end ? base + e * step : end - 1);
-      xp[e] = p.value(i);
-      xq[e] = minus == 1 ? q.value(i) : 0.f;
+      const int32_t at = ALL || i + e * step < end ? i + e * step : end - 1;
+      xp[e] = p.value(at);
+      xq[e] = minus == 1 ? q.value(at) : 0.f;
     }
+    if constexpr (!ALL) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) xp[e] = base + e * step < end ? xp[e] : -INFINITY;
+      for (int e = 0; e < N; ++e) xp[e] = i + e * step < end ? xp[e] : -INFINITY;
+    }
   }
 };
 
@@ -531,19 +535,18 @@ __device__ __forceinline__ VerifyEnd<T> verify_end(const VerifyArgs& a, const do
   const SampleKept* const draft_kept = a.kept + (int64_t)a.batch * a.width;
   if (threadIdx.x < kWave) {
     bool good = false;
-    if (i < n_draft) {
-      const int32_t x = a.drafted[b * w1 + i];
+    if (i < w1) {            // all drafts' loads at once, whatever their number
+      const int32_t x = a.drafted[b * w1 + i], at = x >= 0 && x < a.vocab ? x : 0;
       const float u_in = a.u_accept[b * w1 + i];
       const double u = u_in > 0.f ? fminf(u_in, 0x1.fffffep-1f) : 0.f;
-      if (x >= 0 && x < a.vocab) {
-        const VerifyRow<T> p = verify_row<T>(a, a.target, a.target_ld, b * a.width + i, a.kept, b);
-        const double g = (double)p.weight(table, p.value(x), (uint32_t)x);
-        double h = 1.0, all = 1.0;
-        if (a.draft) {
-          const VerifyRow<T> q = verify_row<T>(a, a.draft, a.draft_ld, b * w1 + i, draft_kept, b);
-          h = (double)q.weight(table, q.value(x), (uint32_t)x);
-          all = (double)q.kept.total;
-        }
+      const VerifyRow<T> p = verify_row<T>(a, a.target, a.target_ld, b * a.width + i, a.kept, b);
+      VerifyRow<T> q = p;
+      if (a.draft) q = verify_row<T>(a, a.draft, a.draft_ld, b * w1 + i, draft_kept, b);
+      const float xp = p.value(at), xq = a.draft ? q.value(at) : 0.f;
+      if (i < n_draft && x == at) {
+        const double g = (double)p.weight(table, xp, (uint32_t)x);
+        const double h = a.draft ? (double)q.weight(table, xq, (uint32_t)x) : 1.0;
+        const double all = a.draft ? (double)q.kept.total : 1.0;
         good = u * h * (double)p.kept.total < g * all;
       }
     }
@@ -582,17 +585,24 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sums_kernel(const Verif
   verify_table(table, a.shift);
   __syncthreads();
   const VerifyEnd<T> e = verify_end<T>(a, table, b, n_draft, &accepted);
-  const int64_t i0 = (int64_t)part * a.per_part;
-  const int32_t i1 = (int32_t)min(i0 + a.per_part, (int64_t)a.vocab);
+  const int32_t i0 = min(part * a.per_part, a.vocab);          // (2^24 tokens at most)
+  int32_t i1 = min(i0 + a.per_part, a.vocab);
   uint64_t sum = 0, own_sum = 0;
+  if (e.p.kept.one) {                     // one token alone, whose index is known
+    const int32_t i = (int32_t)~(uint32_t)e.p.kept.cut;
+    if (threadIdx.x % kWave == 0 && i >= i0 && i < i1) sum = e.weight(table, i, e.p.value(i), e.minus == 1 ? e.q.value(i) : 0.f, own_sum);
+    i1 = 0;
+  }
   constexpr int N = 8;                    // tokens of a lane at a time
-  for (int64_t base = i0 + threadIdx.x % kWave; base - threadIdx.x % kWave < i1; base += N * kWave) {
+  const int32_t lane = threadIdx.x % kWave;
+  for (int32_t base = i0; base < i1; base += N * kWave) {
     float xp[N], xq[N];
-    e.template values<N>(base, kWave, i1, xp, xq);
+    if (base + N * kWave <= i1) e.template values<N, true>(base + lane, kWave, i1, xp, xq);
+    else e.template values<N, false>(base + lane, kWave, i1, xp, xq);
 #pragma unroll
     for (int q = 0; q < N; ++q) {
       uint64_t own;
-      sum += e.weight(table, (int32_t)(base + q * kWave), xp[q], xq[q], own);
+      sum += e.weight(table, base + lane + q * kWave, xp[q], xq[q], own);
       own_sum += own;
     }
   }
@@ -660,22 +670,22 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_draw_kernel(const Verif
   }
   __syncthreads();
   // The first token of it at which the running weight exceeds the target.
-  const int64_t i0 = (int64_t)s_part * a.per_part, i1 = min(i0 + a.per_part, (int64_t)a.vocab);
+  const int32_t i0 = min(s_part * a.per_part, a.vocab), i1 = min(i0 + a.per_part, a.vocab);
   uint64_t seen = total > 0 ? s_before : 0;
-  for (int64_t base = i0; base < i1 && total > 0; base += kVerifyThreads * E) {
+  for (int32_t base = i0; base < i1 && total > 0; base += kVerifyThreads * E) {
     uint64_t g[E], sum = 0, all;
     float xp[E], xq[E];
-    e.template values<E>(base + tid * E, 1, i1, xp, xq);
+    e.template values<E, false>(base + tid * E, 1, i1, xp, xq);
 #pragma unroll
     for (int q = 0; q < E; ++q) {
       uint64_t own_g;
-      g[q] = e.weight(table, (int32_t)(base + tid * E + q), xp[q], xq[q], own_g);
+      g[q] = e.weight(table, base + tid * E + q, xp[q], xq[q], own_g);
       sum += g[q];
     }
     uint64_t at = seen + verify_scan(sum, sums, all) - sum;
 #pragma unroll
     for (int q = 0; q < E; ++q) {
-      if (at <= target && at + g[q] > target) token = (int32_t)(base + tid * E + q);
+      if (at <= target && at + g[q] > target) token = base + tid * E + q;
       at += g[q];
     }
     seen += all;
