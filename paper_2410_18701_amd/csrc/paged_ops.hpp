@@ -69,19 +69,14 @@ struct PagedStepArgs {
 
 constexpr int kStepThreads = 512;        // == BATON_MAX_BATCH: a thread per slot
 
-// Exclusive prefix sum over the workgroup's threads, and the whole.
-__device__ __forceinline__ int32_t step_scan(int32_t x, int32_t* sums, int32_t& total) {
+// Exclusive prefix sum over the workgroup's threads, and the whole.  `sums` alternate, so
+// that one barrier does.
+__device__ __forceinline__ uint64_t step_scan(uint64_t x, uint64_t* sums, uint64_t& total) {
   const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
-  int32_t y = x;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int32_t z = __shfl_up(y, d, kWave);
-    if (lane >= d) y += z;
-  }
-  __syncthreads();
+  const uint64_t y = wave_scan(x);
   if (lane == kWave - 1) sums[w] = y;
   __syncthreads();
-  int32_t before = 0;
+  uint64_t before = 0;
   total = 0;
 #pragma unroll
   for (int v = 0; v < kStepThreads / kWave; ++v) {
@@ -108,7 +103,7 @@ __device__ __forceinline__ int32_t step_find(const int32_t* first, int32_t n, in
 // of (slot, block) whatever order the threads run in.  Bound by the latency of its few
 // dependent reads and barriers.
 __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedStepArgs a) {
-  __shared__ int32_t sums[kStepThreads / kWave];
+  __shared__ uint64_t sums[3][kStepThreads / kWave];
   __shared__ int32_t first_back[kStepThreads + 1], first_more[kStepThreads + 1], first_item[kStepThreads + 1];
   __shared__ int32_t r1[kStepThreads], n1[kStepThreads], r2[kStepThreads], s_had[kStepThreads];
   __shared__ int32_t s_len[kStepThreads], s_new[kStepThreads], s_sink[kStepThreads], s_skip[kStepThreads];
@@ -152,24 +147,21 @@ __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedSte
   const int32_t c1 = max(a1 - a0, 0), c2 = max(covered - b0, 0);
   const int32_t had = leaves ? 0 : min(covered, want);
   const int32_t need = slot ? max(want - had, 0) : 0;
-  int32_t n_back, n_need, n_more;
-  first_back[b] = step_scan(slot ? c1 + c2 : 0, sums, n_back);
+  // Sums of two and three numbers at once: pages and blocks are fewer than 2^26 (a pool
+  // has fewer than 2^31 tokens), needs up to 2^20 a slot.
+  uint64_t all;
+  const bool fits_table = want <= a.max_pages;      // a slot that needs more has none
+  const uint64_t before = step_scan((uint64_t)(slot ? c1 + c2 : 0) << 32 | (fits_table ? need : 0), sums[0], all);
+  const int32_t n_back = (int32_t)(all >> 32);
+  first_back[b] = (int32_t)(before >> 32);
   r1[b] = a0;
   n1[b] = c1;
   r2[b] = b0;
   const int32_t free_now = count + n_back;
-  // A slot's pages are taken if all of the slots up to it fit.  Sums are of at most
-  // max_pages each: a slot that needs more has none.
-  const bool fits_table = want <= a.max_pages;
-  const int32_t before = step_scan(fits_table ? need : 0, sums, n_need);
-  const bool granted = fits_table && (need == 0 || before + need <= free_now);
-  first_more[b] = step_scan(granted ? need : 0, sums, n_more);
+  // A slot's pages are taken if those of all slots up to it fit.
+  const bool granted = fits_table && (need == 0 || (int32_t)(uint32_t)before + need <= free_now);
   s_had[b] = had;
   const int32_t now = granted ? fresh : 0;
-  if (b == 0) {
-    first_back[kStepThreads] = n_back;
-    first_more[kStepThreads] = n_more;
-  }
   // Visible blocks of 32 tokens, and work items.
   int32_t blocks = 0, sink = 0, skip = 0;
   if (slot && now > 0 && now <= kPagedMaxNew) {       // (a prompt comes with its attention done)
@@ -184,18 +176,24 @@ __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedSte
   s_sink[b] = sink;
   s_skip[b] = skip;
   s_blocks[b] = blocks;
+  const bool rows = blocks > 0 && now * a.group > 16;
+  const uint64_t taken = step_scan((uint64_t)(granted ? need : 0) << 38 | (uint64_t)blocks << 11 | (uint64_t)(blocks > 0), sums[1], all);
+  const int32_t n_more = (int32_t)(all >> 38), n_blocks = (int32_t)(all >> 11 & 0x7FFFFFF), n_live = (int32_t)(all & 0x7FF);
+  first_more[b] = (int32_t)(taken >> 38);
   // Items of `per` blocks, so that there are about as many as the launch has workgroups: a
   // live slot's last one is half full.
-  int32_t n_blocks, n_live, n_items;
-  step_scan(blocks, sums, n_blocks);
-  step_scan(blocks > 0, sums, n_live);
-  const bool many = __syncthreads_or(blocks > 0 && now * a.group > 16);
+  const bool many = __syncthreads_or(rows);
   const int32_t target = (many ? kPagedRowItems : kPagedItems) / a.n_kv_heads;
   const int32_t whole = max(target - n_live / 2, target / 4 + 1);
   const int32_t per = max(kPagedMinBlocks, (n_blocks + whole - 1) / whole);
   const int32_t items = (blocks + per - 1) / per;
-  first_item[b] = step_scan(items, sums, n_items);
-  if (b == 0) first_item[kStepThreads] = n_items;
+  first_item[b] = (int32_t)step_scan(items, sums[2], all);
+  const int32_t n_items = (int32_t)all;
+  if (b == 0) {
+    first_back[kStepThreads] = n_back;
+    first_more[kStepThreads] = n_more;
+    first_item[kStepThreads] = n_items;
+  }
   __syncthreads();
 
   int32_t* const stack = a.state + a.at.stack;
