@@ -45,6 +45,15 @@ def _cur_stream():
     return raw(torch._C._cuda_getDevice())
 
 
+def _cur_device():
+    """The current device's index (without torch.cuda.current_device's checks where there is a context)."""
+    import torch
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    if get is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_device()
+    return get()
+
+
 class BatonCache:
     """A batch of `batch` slots over a K/V ring of `capacity` columns per row.
 

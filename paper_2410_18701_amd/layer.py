@@ -12,15 +12,14 @@ beside the projections, and its sampling parameters for the next token.
 import ctypes
 
 from . import baton as B
-from .cache import _cur_stream as _stream
+from .cache import _cur_device, _cur_stream as _stream
 
 
 def _on_this_gpu(what, *tensors):
     """The calls go to the current device's stream: tensors elsewhere are refused."""
-    import torch
-    here = torch.cuda.current_device()
+    here = _cur_device()
     for t in tensors:
-        if t is not None and t.device.index != here:
+        if t is not None and t.get_device() != here:
             raise ValueError(f"{what}: a tensor on {t.device}, the current device is cuda:{here}")
 
 
@@ -162,13 +161,19 @@ def silu_mul(gate_up, out):
 
 
 def rope_qkv(cache, qkv, q, k_new, v_new, theta):
+    """Of a PagedCache, qkv has its width's rows per slot."""
+    paged = hasattr(cache, "desc")
+    rows = cache.batch * (cache.width if paged else 1)
     width = (cache.n_q_heads + 2 * cache.n_kv_heads) * cache.head_dim
-    if tuple(qkv.shape) != (cache.batch, width):
+    if tuple(qkv.shape) != (rows, width):
         raise ValueError("rope_qkv: qkv must be [batch][(Hq + 2 Hkv) * head_dim]")
-    if q.numel() != cache.batch * cache.n_q_heads * cache.head_dim or \
-            k_new.numel() != cache.batch * cache.n_kv_heads * cache.head_dim or v_new.numel() != k_new.numel():
+    if q.numel() != rows * cache.n_q_heads * cache.head_dim or \
+            k_new.numel() != rows * cache.n_kv_heads * cache.head_dim or v_new.numel() != k_new.numel():
         raise ValueError("rope_qkv: output sizes do not match the cache")
-    B.baton_rope_qkv(cache.handle, qkv, q, k_new, v_new, theta, _stream())
+    if paged:
+        B.baton_paged_rope_qkv(cache.desc, qkv, cache.width, q, k_new, v_new, theta, _stream())
+    else:
+        B.baton_rope_qkv(cache.handle, qkv, q, k_new, v_new, theta, _stream())
 
 
 class Sampler:
@@ -259,7 +264,9 @@ class Verifier:
 
 
 class DecodeLayers:
-    """The layers of one model over one BatonCache, with preallocated activations.
+    """The layers of one model over one BatonCache, or over one PagedCache, whose steps have
+    its width's rows for each slot (x [batch * width][hid]: the next token and drafted ones
+    behind it; batch * width <= 256), with preallocated activations.
 
     weights[layer]: dict of bf16 device tensors norm1 [hid], qkv [(Hq + 2 Hkv) D][hid],
     o [hid][Hq D], norm2 [hid], gate_up [2 F][hid], down [hid][F].  The projections
@@ -273,16 +280,19 @@ class DecodeLayers:
     Hkv D], gate_up in [F, F], the same adapter at the same index everywhere);
     slot_adapter[slot] is the index its query uses, -1 for none, and may be changed
     between steps (a captured step keeps the indices that it was captured with).  head: dict
-    of norm [hid] and out [vocab][hid] (vocab a multiple of 8), for next_tokens."""
+    of norm [hid] and out [vocab][hid] (vocab a multiple of 8), for next_tokens, or
+    accept_drafts over a PagedCache."""
 
     PROJ = ("qkv", "o", "gate_up", "down")
 
     def __init__(self, cache, weights, gemm, theta=10000.0, eps=1e-5, adapters=None, head=None):
         import torch
         self.cache, self.w, self.gemm, self.theta, self.eps = cache, weights, gemm, theta, eps
-        Bt, Hq, Hkv, D = cache.batch, cache.n_q_heads, cache.n_kv_heads, cache.head_dim
+        Hq, Hkv, D = cache.n_q_heads, cache.n_kv_heads, cache.head_dim
+        self.width = getattr(cache, "width", 1)
+        Bt = cache.batch * self.width
         if Bt > B.BATON_GEMM_MAX_ROWS:
-            raise ValueError(f"at most {B.BATON_GEMM_MAX_ROWS} slots")
+            raise ValueError(f"at most {B.BATON_GEMM_MAX_ROWS} slots (times their new tokens)")
         self.wp = [{k: gemm.pack(w[k]) for k in self.PROJ} for w in weights]
         hid = weights[0]["norm1"].numel()
         F = weights[0]["down"].shape[1]
@@ -293,24 +303,28 @@ class DecodeLayers:
         self._normed = None   # (layer, x) whose norm1 input h already holds
         if adapters is not None and (len(adapters) != len(weights) or any(set(a) - set(self.PROJ) for a in adapters)):
             raise ValueError(f"adapters: one dict over {self.PROJ} per layer")
-        self.adapters, self.slot_adapter = adapters, [-1] * Bt
+        self.adapters, self.slot_adapter = adapters, [-1] * cache.batch
         self.head = None
         if head is not None:
             vocab = head["out"].shape[0]
             self.head, self.head_norm = gemm.pack(head["out"]), head["norm"]
-            self.logits, self.sampler = e(Bt, vocab), Sampler(Bt, vocab)
+            self.logits = e(Bt, vocab)
+            self.sampler = Sampler(Bt, vocab) if self.width == 1 else None
+            self.verifier = Verifier(cache.batch, self.width, vocab) if hasattr(cache, "desc") else None
 
     def _adapt(self, layer, proj, x, y):
         """y += the low-rank products of the slots with an adapter of this projection."""
         ad = self._adapter(layer, proj)
         if ad is not None:
-            self.gemm.linear_adapters(x, ad, self.slot_adapter, y, accumulate=True)
+            rows = self.slot_adapter if self.width == 1 else [i for i in self.slot_adapter for _ in range(self.width)]
+            self.gemm.linear_adapters(x, ad, rows, y, accumulate=True)
 
     def _adapter(self, layer, proj):
         return None if self.adapters is None or max(self.slot_adapter) < 0 else self.adapters[layer].get(proj)
 
     def layer(self, layer, x):
-        """One layer of the decode step on the residual stream x [batch][hid] (in place)."""
+        """One layer of the decode step on the residual stream x [batch][hid] (a PagedCache:
+        [batch * width][hid]; in place)."""
         w, wp, g = self.w[layer], self.wp[layer], self.gemm
         if self._normed != (layer, x.data_ptr()):   # h holds norm1(x) after the previous layer
             rmsnorm(x, w["norm1"], self.h, self.eps)
@@ -341,9 +355,23 @@ class DecodeLayers:
         """The next token of every slot (int32 [batch], the Sampler's own tensor; a free
         slot's says nothing) from the last layer's residual stream x [batch][hid]: norm,
         vocabulary projection, sampling with each slot's parameters and random number u."""
-        if self.head is None:
-            raise ValueError("next_tokens: no head was given")
+        if self.head is None or self.sampler is None:
+            raise ValueError("next_tokens: no head was given" if self.head is None else
+                             "next_tokens: one new token per slot (accept_drafts takes several)")
+        return self.sampler(self._logits(x), u, temperature, top_k, top_p, min_p)
+
+    def _logits(self, x):
         rmsnorm(x, self.head_norm, self.h, self.eps)
         self._normed = None
-        self.gemm.linear_packed(self.h, self.head, self.logits)
-        return self.sampler(self.logits, u, temperature, top_k, top_p, min_p)
+        return self.gemm.linear_packed(self.h, self.head, self.logits)
+
+    def accept_drafts(self, x, draft, drafted, n_draft, u_accept, u_token, temperature=None, top_k=None, top_p=None,
+                      min_p=None):
+        """Over a PagedCache: the drafted tokens that are accepted and the token behind them
+        (tokens [batch][width], n_out [batch], the Verifier's own tensors) from the last layer's
+        residual stream x [batch * width][hid], whose row b width + i belongs to slot b's i-th
+        new token; the other arguments as Verifier's.  n_out is the next begin's keep."""
+        if self.head is None or self.verifier is None:
+            raise ValueError("accept_drafts: no head was given" if self.head is None else "accept_drafts: a PagedCache only")
+        logits = self._logits(x).view(self.cache.batch, self.width, -1)
+        return self.verifier(logits, draft, drafted, n_draft, u_accept, u_token, temperature, top_k, top_p, min_p)

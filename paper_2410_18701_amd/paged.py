@@ -55,13 +55,12 @@ class PagedCache:
         import torch
         if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
             raise ValueError(f"PagedCache: {what} must be {n} contiguous int32 values")
-        _on_this_gpu("PagedCache", t, self.lens)
 
     def reset(self, order=None):
         """Every slot free, every page in the pool."""
         if order is not None:
             self._numbers("order", order, self.n_pages)
-        _on_this_gpu("PagedCache", self.lens)
+        _on_this_gpu("PagedCache", self.lens, order)
         B.baton_paged_reset(self.desc, order, _cur_stream())
 
     def begin(self, n_new, keep=None):
@@ -70,6 +69,7 @@ class PagedCache:
         self._numbers("n_new", n_new, self.batch)
         if keep is not None:
             self._numbers("keep", keep, self.batch)
+        _on_this_gpu("PagedCache", self.lens, n_new, keep)
         B.baton_paged_step(self.desc, keep, n_new, self.slot_map, self.width, self.width, self.missing, _cur_stream())
         return self.slot_map
 
