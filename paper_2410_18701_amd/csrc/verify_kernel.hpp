@@ -511,19 +511,17 @@ struct VerifyEnd {
     const double d = (double)own * cp - (double)h * cq;
     return d > 0.0 ? sample_whole(d) : 0;
   }
-  // The logits of N tokens from `i` on, `step` apart; ALL: below `end` (the others' are -inf).
-  template <int N, bool ALL>
+  // The logits of N tokens from `i` on, `step` apart, below `end` (the others' are -inf).
+  template <int N>
   __device__ __forceinline__ void values(int32_t i, int32_t step, int32_t end, float (&xp)[N], float (&xq)[N]) const {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const int32_t at = ALL || i + e * step < end ? i + e * step : end - 1;
+      const int32_t at = i + e * step < end ? i + e * step : end - 1;
       xp[e] = p.value(at);
       xq[e] = minus == 1 ? q.value(at) : 0.f;
     }
-    if constexpr (!ALL) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) xp[e] = i + e * step < end ? xp[e] : -INFINITY;
-    }
+    for (int e = 0; e < N; ++e) xp[e] = i + e * step < end ? xp[e] : -INFINITY;
   }
 };
 
@@ -593,12 +591,41 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sums_kernel(const Verif
     if (threadIdx.x % kWave == 0 && i >= i0 && i < i1) sum = e.weight(table, i, e.p.value(i), e.minus == 1 ? e.q.value(i) : 0.f, own_sum);
     i1 = 0;
   }
-  constexpr int N = 8;                    // tokens of a lane at a time
   const int32_t lane = threadIdx.x % kWave;
-  for (int32_t base = i0; base < i1; base += N * kWave) {
+  // Rows that start at 16 bytes: V vectors of a lane at a time (parts begin at whole ones).
+  constexpr int EPV = Lane16<T>::kElems, V = 4;
+  int32_t base = i0;
+  if (((reinterpret_cast<uintptr_t>(e.p.row) | (e.minus == 1 ? reinterpret_cast<uintptr_t>(e.q.row) : 0)) & 15u) == 0) {
+    const int32_t end = i1 > i0 ? i0 + (i1 - i0) / EPV * EPV : i0;
+    for (; base < end; base += V * EPV * kWave) {
+      u32x4 vp[V], vq[V];
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const int32_t at = min(base + (q * kWave + lane) * EPV, end - EPV) / EPV;
+        vp[q] = reinterpret_cast<const u32x4*>(e.p.row)[at];
+        vq[q] = e.minus == 1 ? reinterpret_cast<const u32x4*>(e.q.row)[at] : u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const int32_t i = base + (q * kWave + lane) * EPV;
+        if (i >= end) continue;
+        float xp[EPV], xq[EPV];
+        Lane16<T>::widen(vp[q], xp);
+        Lane16<T>::widen(vq[q], xq);
+#pragma unroll
+        for (int k = 0; k < EPV; ++k) {
+          uint64_t own;
+          sum += e.weight(table, i + k, xp[k], xq[k], own);
+          own_sum += own;
+        }
+      }
+    }
+    base = end;
+  }
+  constexpr int N = 8;                    // tokens of a lane at a time
+  for (; base < i1; base += N * kWave) {
     float xp[N], xq[N];
-    if (base + N * kWave <= i1) e.template values<N, true>(base + lane, kWave, i1, xp, xq);
-    else e.template values<N, false>(base + lane, kWave, i1, xp, xq);
+    e.template values<N>(base + lane, kWave, i1, xp, xq);
 #pragma unroll
     for (int q = 0; q < N; ++q) {
       uint64_t own;
@@ -675,7 +702,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_draw_kernel(const Verif
   for (int32_t base = i0; base < i1 && total > 0; base += kVerifyThreads * E) {
     uint64_t g[E], sum = 0, all;
     float xp[E], xq[E];
-    e.template values<E, false>(base + tid * E, 1, i1, xp, xq);
+    e.template values<E>(base + tid * E, 1, i1, xp, xq);
 #pragma unroll
     for (int q = 0; q < E; ++q) {
       uint64_t own_g;
