@@ -197,17 +197,18 @@ __device__ __forceinline__ uint32_t value_place(uint32_t w) { return w ^ (w >> 3
 
 // Prefix sum over the workgroup's 16 waves, exclusive, and the whole.
 __device__ __forceinline__ uint64_t value_scan(uint64_t x, uint64_t* shared, uint64_t& total) {
+  const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const uint64_t y = wave_scan(x);
   __syncthreads();
-  if (threadIdx.x % kWave == kWave - 1) shared[threadIdx.x / kWave] = y;
+  if (lane == kWave - 1) shared[w] = y;
   __syncthreads();
-  total = 0;
-  uint64_t before = 0;
-  for (int v = 0; v < kSampleWaves; ++v) {
-    before += v < (int)(threadIdx.x / kWave) ? shared[v] : 0;
-    total += shared[v];
-  }
-  return before + y - x;
+  const uint64_t t = wave_scan(lane < kSampleWaves ? shared[lane] : 0);    // lane l: up to wave l
+  auto from = [&](int l) {
+    return (uint64_t)__builtin_amdgcn_readlane((int)(t >> 32), l) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)t, l);
+  };
+  total = from(kSampleWaves - 1);
+  return y - x + (w > 0 ? from(w - 1) : 0);
 }
 
 // False (for all threads): a value is there too often for its counter.
@@ -297,7 +298,8 @@ __device__ __forceinline__ bool verify_values_row(ValueShared& s, const VerifyLo
   __syncthreads();
   const uint64_t count = s.n[block], sum = s.sum[block];
   uint64_t all_count, kept, kept_high = 0;
-  for (int v = 0; v < kSampleWaves; ++v) kept_high += s.high[v];
+  if (want_m)
+    for (int v = 0; v < kSampleWaves; ++v) kept_high += s.high[v];
   const uint64_t count_before = value_scan(count, s.scan, all_count);
   const uint64_t sum_before = value_scan(sum, s.scan, kept);
   bool cut = false;
