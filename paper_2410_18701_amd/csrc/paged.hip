@@ -236,7 +236,10 @@ baton_status baton_paged_attn(const baton_paged_desc* d, int32_t layer, const vo
   const size_t need = baton_paged_attn_workspace_bytes(d, width);
   if (need && (!ws || !aligned(ws, 16) || ws_bytes < need)) return BATON_EINVAL;
   const int32_t items = max_items(*d);
-  if ((int64_t)items * d->n_kv_heads >= (int64_t(1) << 24)) return BATON_EINVAL;   // fewer than 2^32 threads
+  // launches of fewer than 2^32 threads
+  if ((int64_t)items * d->n_kv_heads >= (int64_t(1) << 24) ||
+      (int64_t)d->batch * d->n_q_heads * width >= (int64_t(1) << 24))
+    return BATON_EINVAL;
   baton::PagedAttnArgs a;
   std::memset(&a, 0, sizeof(a));
   a.q = static_cast<const uint8_t*>(q);

@@ -66,6 +66,8 @@ baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, 
       !aligned(u_accept, 4) || !aligned(u_token, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) ||
       !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(tokens, 4) || !aligned(n_out, 4))
     return BATON_EINVAL;
+  // launches of fewer than 2^32 threads (logits of 256 GiB and more)
+  if ((int64_t)batch * (2 * width - 1) * row_pieces(vocab, (int32_t)es) >= (int64_t(1) << 24)) return BATON_EINVAL;
   if (!ws || !aligned(ws, 16) || ws_bytes < baton_verify_workspace_bytes(batch, width, vocab)) return BATON_EINVAL;
   baton::VerifyArgs a;
   std::memset(&a, 0, sizeof(a));

@@ -205,6 +205,38 @@ def test_long_queries_are_divided(dtype, d, width):
     assert int(t.c._state[1]) > 60                          # work items
 
 
+@pytest.mark.parametrize("hq,hkv,width", [(2, 1, 1), (8, 8, 4), (8, 1, 3)])
+def test_the_largest_batch(hq, hkv, width):
+    r = np.random.default_rng(hq)
+    lens = [int(x) for x in r.integers(0, 300, 512)]
+    t = Twin(17, batch=512, hq=hq, hkv=hkv, d=64, page=32, width=width, lens=lens, max_pages=16)
+    n_new = [int(x) for x in r.integers(0, width + 1, 512)]
+    t.first(n_new)
+    ks, vs = t.c.extract([5, 511], [lens[5] + n_new[5], lens[511] + n_new[511]])      # the new tokens are in the pages
+    assert torch.equal(ks[0], t.ks[5]) and torch.equal(vs[1], t.vs[511])
+
+
+@pytest.mark.parametrize("hq,width,lens", [(32, 1, [70000] * 7 + [65000]), (64, 16, [40000])])
+def test_items_of_many_blocks(hq, width, lens):
+    """Items of more than 64 blocks a wave (and a workgroup's), whose pages are looked up in turns."""
+    g = torch.Generator(device="cuda").manual_seed(18)
+    batch, hkv, d = len(lens), 32, 64
+    c = PagedCache(1, batch, hq, hkv, d, sum(-(-(n + width) // 128) for n in lens), 600, page=128, width=width)
+    c.begin(i32(lens))
+    ks, vs = ([rand(g, 1, hkv, n, d) for n in lens] for _ in range(2))
+    c.embed(list(range(batch)), lens, ks, vs)
+    c.begin(i32([width] * batch), keep=i32(lens))
+    q, k, v = rand(g, batch, width, hq, d), rand(g, batch, width, hkv, d), rand(g, batch, width, hkv, d)
+    out = c.decode_attn(0, q, k, v, out=torch.zeros_like(q))
+    assert int(c._state[1]) * 64 * (4 if width == 1 else 1) < sum(-(-n // 32) for n in lens)     # work items
+    for b in (0, batch - 1):
+        for h in (0, 31):
+            kk, vv = (torch.cat([x[b][0, h], y[b, :, h]])[None] for x, y in ((ks, k), (vs, v)))
+            heads = slice(h * hq // hkv, (h + 1) * hq // hkv)
+            want = O.attention(f64(q[b, :, heads]), f64(kk), f64(vv), lens[b])
+            close(out[b, :, heads], want, float(vv.abs().max()), "bf16")
+
+
 def test_offsets_past_32_bits():
     """A pool of 2^31 and more elements, a query in its last pages."""
     n_pages = 33 * 2 ** 31 // (8 * 256 * 128) // 32

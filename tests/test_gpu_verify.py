@@ -155,6 +155,23 @@ def test_equal_logits():
         check(target, draft, torch.full((batch, 1), x, dtype=torch.int32, device="cuda"), None, u[:, None].contiguous(), u, params)
 
 
+def test_a_value_of_more_tokens_than_its_counter_holds():
+    """bf16 rows are counted by value in 16 bits: rows in which one value is there 65,536 times and more."""
+    batch, vocab = 5, 140001
+    g = torch.Generator(device="cuda").manual_seed(12)
+    target = torch.zeros((batch, 2, vocab), dtype=torch.bfloat16, device="cuda")
+    target[1] = torch.where(torch.rand((2, vocab), generator=g, device="cuda") < 0.9, 1.5, 2.0)
+    target[2, :, :65536] = 1.0
+    target[3, :, 70000:] = -0.0
+    target[4] = torch.where(torch.rand((2, vocab), generator=g, device="cuda") < 0.3, 1.0, -float("inf"))
+    draft = (target[:, :1] + torch.randn((batch, 1, vocab), generator=g, device="cuda")).bfloat16()
+    params = [dict(top_p=0.6), dict(top_k=9000), dict(top_p=0.95), dict(top_k=90000, top_p=0.5), dict(min_p=0.5, top_p=0.9)]
+    for u in (0.11, 0.73):
+        ut = torch.full((batch,), u, device="cuda")
+        for x in (3, 100000):
+            check(target, draft, torch.full((batch, 1), x, dtype=torch.int32, device="cuda"), None, ut[:, None].contiguous(), ut, params)
+
+
 def test_tokens_are_distributed_as_the_target():
     """Over 512 x 40 draws the first token's frequencies are p's within five deviations."""
     g = torch.Generator(device="cuda").manual_seed(8)

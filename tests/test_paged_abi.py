@@ -94,6 +94,7 @@ def attn(d=None, layer=0, q=Q, k=Q, v=Q, width=1, out=O_, scale=0.0, ws=W, ws_by
 @pytest.mark.parametrize("kw", [
     dict(layer=2), dict(layer=-1), dict(q=0), dict(out=0), dict(k=0), dict(v=0), dict(q=Q + 8), dict(k=Q + 2),
     dict(v=Q + 4), dict(out=O_ + 8), dict(width=0), dict(width=17), dict(d=desc(n_q_heads=16), width=9),
+    dict(d=desc(batch=512, n_q_heads=1 << 16, n_kv_heads=1 << 16, n_pages=1, layer_stride=0, v=1 << 40), ws_bytes=1 << 60),
     dict(scale=float("inf")), dict(scale=float("nan")), dict(ws=0), dict(ws=W + 8), dict(ws_bytes=16)],
     ids=lambda kw: "-".join(kw))
 def test_attention_refusals(kw):

@@ -28,7 +28,8 @@ def status(dtype=B.BATON_BF16, target=X, target_ld=100, draft=Y, draft_ld=100, b
     dict(width=17), dict(vocab=0), dict(vocab=(1 << 24) + 1, target_ld=1 << 25, draft_ld=1 << 25), dict(drafted=0),
     dict(drafted=Z + 2), dict(n_draft=Z + 1), dict(u_accept=0), dict(u_accept=Z + 2), dict(u_token=0), dict(tokens=0),
     dict(tokens=Z + 1), dict(n_out=0), dict(n_out=Z + 2), dict(temperature=Z + 1), dict(top_k=Z + 2), dict(top_p=Z + 3),
-    dict(min_p=Z + 1), dict(ws=0), dict(ws=W + 8), dict(ws_bytes=64)], ids=lambda kw: "-".join(kw))
+    dict(min_p=Z + 1), dict(ws=0),
+    dict(batch=512, width=16, vocab=1 << 24, target_ld=1 << 24, draft_ld=1 << 24, dtype=B.BATON_F32, ws_bytes=1 << 60), dict(ws=W + 8), dict(ws_bytes=64)], ids=lambda kw: "-".join(kw))
 def test_refusals(kw):
     assert status(**kw) == B.BATON_EINVAL
 
