@@ -253,7 +253,9 @@ baton_status baton_paged_attn(const baton_paged_desc* d, int32_t layer, const vo
   a.state = d->state;
   a.at = state_at(*d);
   a.partial = static_cast<float*>(ws);
-  a.qscale = (float)((scale == 0.f ? 1.0 / std::sqrt((double)d->head_dim) : (double)scale) * 1.4426950408889634074);
+  const double qscale = (scale == 0.f ? 1.0 / std::sqrt((double)d->head_dim) : (double)scale) * 1.4426950408889634074;
+  a.qscale = (float)qscale;
+  a.qscale_rest = (float)(qscale - (double)a.qscale);
   a.batch = d->batch;
   a.n_kv_heads = d->n_kv_heads;
   a.group = group;

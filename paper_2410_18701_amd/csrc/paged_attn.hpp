@@ -44,7 +44,7 @@ struct PagedAttnArgs {
   const int32_t* state;
   PagedState at;
   float* partial;          // [item][head][rows]: D sums, maximum, sum of the weights
-  float qscale;            // scale * log2 e
+  float qscale, qscale_rest;   // scale * log2 e, and what it is more than that
   int32_t batch, n_kv_heads, group, width, max_pages, n_pages, page_shift, window, sinks;
 };
 
@@ -64,23 +64,25 @@ template <typename T, int D>
 __device__ __forceinline__ void paged_append(const PagedAttnArgs& a, const PagedItem& it, int32_t h, int32_t block,
                                              uint8_t* kb, uint8_t* vb, int lane) {
   using Geo = PagedGeo<T, D>;
-  const int32_t j0 = max(it.len, block * kPagedBlock), j1 = min(it.len + it.n_new, (block + 1) * kPagedBlock);
-  for (int32_t j = j0; j < j1; ++j) {
-    const int32_t t = j % kPagedBlock;
-    const int64_t row = (((int64_t)it.b * a.width + (j - it.len)) * a.n_kv_heads + h) * Geo::kRow;
-    const int tl = (t >> 2) & 1, g = t >> 3, i = 4 * g + (t & 3);
-    if (lane < Geo::kRow / 16) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(a.k_new + row + lane * 16);
-      *reinterpret_cast<u32x4*>(kb + (((tl * Geo::kChunks + lane / 4) * 64) + (lane % 4) * 16 + i) * 16) = w;
-    }
-    for (int d = lane; d < D; d += kWave) {
-      if constexpr (T::kBytes == 2)
-        *reinterpret_cast<uint16_t*>(vb + ((d / 16 * 64) + g * 16 + d % 16) * 16 + (t & 7) * 2) =
-            reinterpret_cast<const uint16_t*>(a.v_new + row)[d];
-      else
-        *reinterpret_cast<uint32_t*>(vb + (((tl * Geo::kDt + d / 16) * 64) + g * 16 + d % 16) * 16 + (t & 3) * 4) =
-            reinterpret_cast<const uint32_t*>(a.v_new + row)[d];
-    }
+  constexpr int P = Geo::kRow / 16;
+  const int32_t j0 = max(it.len, block * kPagedBlock), n = min(it.len + it.n_new, (block + 1) * kPagedBlock) - j0;
+  const int64_t row0 = (((int64_t)it.b * a.width + (j0 - it.len)) * a.n_kv_heads + h) * Geo::kRow;
+  const int64_t step = (int64_t)a.n_kv_heads * Geo::kRow;       // from token to token
+#pragma unroll 4
+  for (int32_t idx = lane; idx < n * P; idx += kWave) {
+    const int32_t j = idx / P, p = idx % P, t = (j0 + j) % kPagedBlock;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(a.k_new + row0 + j * step + p * 16);
+    *reinterpret_cast<u32x4*>(kb + ((((t >> 2 & 1) * Geo::kChunks + p / 4) * 64) + (p % 4) * 16 + 4 * (t >> 3) + (t & 3)) * 16) = w;
+  }
+#pragma unroll 4
+  for (int32_t idx = lane; idx < n * D; idx += kWave) {
+    const int32_t j = idx / D, d = idx % D, t = (j0 + j) % kPagedBlock;
+    if constexpr (T::kBytes == 2)
+      *reinterpret_cast<uint16_t*>(vb + ((d / 16 * 64) + (t >> 3) * 16 + d % 16) * 16 + (t & 7) * 2) =
+          reinterpret_cast<const uint16_t*>(a.v_new + row0 + j * step)[d];
+    else
+      *reinterpret_cast<uint32_t*>(vb + ((((t >> 2) & 1) * Geo::kDt + d / 16) * 64 + (t >> 3) * 16 + d % 16) * 16 + (t & 3) * 4) =
+          reinterpret_cast<const uint32_t*>(a.v_new + row0 + j * step)[d];
   }
   __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the stores are done before the block is read
 }
@@ -233,7 +235,7 @@ __device__ __forceinline__ bool paged_odd(const typename PagedGeo<T, D>::Vecs& v
 // What a workgroup's waves know of their item.
 struct PagedRows {
   int32_t len, n_new, group, window, sinks, shift;   // shift: log2 of a page's blocks
-  float qscale;
+  float qscale, qscale_rest;
 
   // Bit e: a token at a position from p0 to p1 sees token j + e.
   __device__ __forceinline__ uint32_t sees(int32_t j, int32_t p0, int32_t p1) const {
@@ -271,26 +273,24 @@ struct PagedTile {
                                       typename PagedGeo<T, D>::Vecs& vw, int g4) {
     const bool whole = there && r.whole(j0);
     const int32_t jl = j0 + 8 * g4;
-    if (whole) {
+    const uint32_t bits = whole ? 0xFFu : there ? r.sees(jl, pos, pos) : 0u;
+    // what no row sees: anything may lie there
+    if (!whole) paged_clear<T, D>(vw, there ? r.sees(jl, r.len, r.len + r.n_new - 1) : 0u);
+    float mx = -INFINITY, p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] *= r.qscale;
-    } else {
-      const uint32_t bits = there ? r.sees(jl, pos, pos) : 0u;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] = (bits >> e) & 1u ? s[e] * r.qscale : -INFINITY;
-      // what no row sees: anything may lie there
-      paged_clear<T, D>(vw, there ? r.sees(jl, r.len, r.len + r.n_new - 1) : 0u);
-    }
-    float mx = s[0], p[8];
-#pragma unroll
-    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
+    for (int e = 0; e < 8; ++e) mx = fmaxf(mx, (bits >> e) & 1u ? s[e] * r.qscale : -INFINITY);
     const float mn = fmaxf(m, max_over_groups(mx));
     const float ref = mn == -INFINITY ? 0.f : mn;       // nothing seen yet
     const float alpha = fast_exp2(m - ref);
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      p[e] = fast_exp2(s[e] - ref);
+      // The difference is rounded, not the score, whose magnitude may be many times as
+      // large (the reference's own rounding is the same for all tokens); in fp32 with the rest
+      // of the scale, which is off by up to 2^-25 of itself.
+      float x = fmaf(s[e], r.qscale, -ref);
+      if constexpr (T::kBytes == 4) x = fmaf(s[e], r.qscale_rest, x);
+      p[e] = (bits >> e) & 1u ? fast_exp2(x) : 0.f;
       sum += p[e];
     }
     m = mn;
@@ -312,10 +312,9 @@ __device__ __forceinline__ void paged_write(const PagedAttnArgs& a, const PagedI
                                             const PagedTile<D>& x, int lane) {
   using Geo = PagedGeo<T, D>;
   const int g4 = lane / 16, c16 = lane % 16;
-  const int32_t parts = a.state[a.at.first + it.b + 1] - a.state[a.at.first + it.b];
   const int32_t G = a.group, r = x.first + c16;
   if (r >= it.n_new * G) return;
-  if (parts == 1) {
+  if (it.parts == 1) {
     const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
     uint8_t* const row = a.out + ((((int64_t)it.b * a.width + r / G) * a.n_kv_heads + h) * G + r % G) * Geo::kRow;
 #pragma unroll
@@ -417,16 +416,18 @@ paged_attn_kernel(const PagedAttnArgs a) {
   __shared__ u32x4 sm[kPagedWaves / 2 * Geo::kDt][kWave];
   __shared__ float sm_m[kPagedWaves][16], sm_l[kPagedWaves][16];
   const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
-  if (item >= a.state[kNumItems]) return;
-  const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];
-  if (it.n_new > a.width) return;          // a prompt: it comes whole, with its attention done
+  const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];   // (the list has room for all)
+  if (item >= a.state[kNumItems] || it.n_new > a.width) return;   // the latter: more than the call brings
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int g4 = lane / 16, c16 = lane % 16;
-  const PagedRows r = {it.len, it.n_new, a.group, a.window, a.sinks, a.page_shift - 5, a.qscale};
+  const PagedRows r = {it.len, it.n_new, a.group, a.window, a.sinks, a.page_shift - 5, a.qscale, a.qscale_rest};
 
   // This wave's blocks: w, w + 4, ... of the item.
   const int32_t n_mine = (it.v1 - it.v0 - w + kPagedWaves - 1) / kPagedWaves;
   auto block_of = [&](int32_t k) { return paged_block_of(it, w + k * kPagedWaves); };
+  u32x4 qw[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) qw[c] = paged_query<T, D>(a, it, h, c16, c, g4);
   if (a.k_new) {       // the new tokens of its blocks (the last ones) first
     for (int32_t k = n_mine - 1; k >= 0 && block_of(k) * kPagedBlock + kPagedBlock > it.len; --k) {
       const int32_t block = block_of(k), id = __builtin_amdgcn_readfirstlane(paged_page(a, it, block, r.shift));
@@ -435,9 +436,6 @@ paged_attn_kernel(const PagedAttnArgs a) {
       paged_append<T, D>(a, it, h, block, a.k + off, a.v + off, lane);
     }
   }
-  u32x4 qw[CH];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) qw[c] = paged_query<T, D>(a, it, h, c16, c, g4);
   PagedTile<D> x(r, 0, c16);
 
   // 64 blocks at a time, whose pages are in a lane each.  K of the next block is asked for
@@ -512,16 +510,18 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_rows_kernel(co
   __shared__ __attribute__((aligned(1024))) u32x4 buf3[R == 4 ? 2 * NV : 1][kWave];
   __shared__ float sm_m[kPagedWaves][16], sm_l[kPagedWaves][16];
   const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
-  if (item >= a.state[kNumItems]) return;
-  const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];
-  if (it.n_new > a.width) return;          // a prompt: it comes whole, with its attention done
+  const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];   // (the list has room for all)
+  if (item >= a.state[kNumItems] || it.n_new > a.width) return;   // the latter: more than the call brings
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int g4 = lane / 16, c16 = lane % 16;
-  const PagedRows r = {it.len, it.n_new, a.group, a.window, a.sinks, a.page_shift - 5, a.qscale};
+  const PagedRows r = {it.len, it.n_new, a.group, a.window, a.sinks, a.page_shift - 5, a.qscale, a.qscale_rest};
   const int32_t n = it.v1 - it.v0, rows = it.n_new * a.group;
   const int32_t tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, groups = kPagedWaves / tiles;
   const int32_t tile = w % tiles, turn = w / tiles;
 
+  u32x4 qw[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) qw[c] = paged_query<T, D>(a, it, h, tile * 16 + c16, c, g4);
   if (a.k_new) {       // the new tokens of the item's blocks (the last ones) first, a wave a block
     for (int32_t k = n - 1; k >= 0 && paged_block_of(it, k) * kPagedBlock + kPagedBlock > it.len; --k) {
       const int32_t block = paged_block_of(it, k), id = __builtin_amdgcn_readfirstlane(paged_page(a, it, block, r.shift));
@@ -531,9 +531,6 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_rows_kernel(co
     }
     __syncthreads();
   }
-  u32x4 qw[CH];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) qw[c] = paged_query<T, D>(a, it, h, tile * 16 + c16, c, g4);
   PagedTile<D> x(r, tile, c16);
 
   // 64 blocks at a time, whose pages are in a lane each.

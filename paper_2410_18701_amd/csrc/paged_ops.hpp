@@ -23,10 +23,10 @@ constexpr int kPagedItems = 2048;        // workgroups of an attention launch, a
 constexpr int kPagedRowItems = 512;      // and with more than 16 rows per head, which two a compute unit fill
 constexpr int kPagedMinBlocks = 8;       // blocks per work item, at least
 
-// A slot's work item: visible blocks v0 .. v1 - 1 of slot b, the `part`-th of `parts`.
+// A work item, one of a slot's `parts`: visible blocks v0 .. v1 - 1 of slot b.
 // Visible block v is the query's block v (v < sink) or v + skip.
 struct PagedItem {
-  int32_t b, v0, v1, part;
+  int32_t b, v0, v1, parts;
   int32_t len, n_new, sink, skip;
 };
 
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedSte
   PagedItem* const list = reinterpret_cast<PagedItem*>(a.state + a.at.items);
   for (int32_t k = threadIdx.x; k < n_items; k += kStepThreads) {
     const int32_t s = step_find(first_item, kStepThreads, k), part = k - first_item[s];
-    list[k] = {s, part * per, min((part + 1) * per, s_blocks[s]), part, s_len[s], s_new[s], s_sink[s], s_skip[s]};
+    list[k] = {s, part * per, min((part + 1) * per, s_blocks[s]), first_item[s + 1] - first_item[s], s_len[s], s_new[s], s_sink[s], s_skip[s]};
   }
   if (!a.slot_map) return;
   __syncthreads();                        // the table's new entries are seen
