@@ -88,34 +88,43 @@ __device__ __forceinline__ void paged_append(const PagedAttnArgs& a, const Paged
 }
 
 // Scores of 32 tokens against 16 rows: s[e] for token 8 (lane / 16) + e of row lane % 16.
+// fp32: four sums per score, so that each has fewer roundings (and waits for fewer of its
+// own products).
 template <typename T, int D>
 __device__ __forceinline__ void paged_scores(const typename PagedGeo<T, D>::Vecs& kw,
                                              const u32x4 (&qw)[PagedGeo<T, D>::kChunks], float (&s)[8]) {
   using Geo = PagedGeo<T, D>;
 #pragma unroll
   for (int tl = 0; tl < 2; ++tl) {
-    pa_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (T::kBytes == 2) {
+      pa_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < Geo::kChunks; ++c) {
-      const u32x4 kk = kw[tl * Geo::kChunks + c], qq = qw[c];
-      if constexpr (T::kBytes == 2) {
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pa_bf16x8, kk),
-                                                      __builtin_bit_cast(pa_bf16x8, qq), acc, 0, 0, 0);
-      } else {
+      for (int c = 0; c < Geo::kChunks; ++c)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pa_bf16x8, kw[tl * Geo::kChunks + c]),
+                                                      __builtin_bit_cast(pa_bf16x8, qw[c]), acc, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[4 * tl + r] = acc[r];
+    } else {
+      pa_f32x4 acc[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = pa_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < Geo::kChunks; ++c)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kk[j]), __uint_as_float(qq[j]), acc, 0, 0, 0);
-      }
-    }
+          acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[tl * Geo::kChunks + c][j]),
+                                                        __uint_as_float(qw[c][j]), acc[j], 0, 0, 0);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s[4 * tl + r] = acc[r];
+      for (int r = 0; r < 4; ++r) s[4 * tl + r] = (acc[0][r] + acc[1][r]) + (acc[2][r] + acc[3][r]);
+    }
   }
 }
 
-// o += V^T P^T over 32 tokens, finite values.
+// o = alpha o + V^T P^T over 32 tokens, finite values.  fp32: the block's sum by itself, so
+// that a long row's has a rounding per block, not per product.
 template <typename T, int D>
 __device__ __forceinline__ void paged_values(const typename PagedGeo<T, D>::Vecs& vw, const float (&p)[8],
-                                             pa_f32x4 (&o)[D / 16]) {
+                                             float alpha, pa_f32x4 (&o)[D / 16]) {
   constexpr int DT = D / 16;
   if constexpr (T::kBytes == 2) {
     pa_bf16x8 hi, lo;
@@ -127,17 +136,20 @@ __device__ __forceinline__ void paged_values(const typename PagedGeo<T, D>::Vecs
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
       const pa_bf16x8 v = __builtin_bit_cast(pa_bf16x8, vw[t]);
+      o[t] *= alpha;
       o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, o[t], 0, 0, 0);
       o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, o[t], 0, 0, 0);
     }
   } else {
 #pragma unroll
-    for (int tl = 0; tl < 2; ++tl)
+    for (int t = 0; t < DT; ++t) {
+      pa_f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int e = 0; e < 8; ++e)
+        x = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[e / 4 * DT + t][e % 4]), p[e], x, 0, 0, 0);
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
-          o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[tl * DT + t][r]), p[4 * tl + r], o[t], 0, 0, 0);
+      for (int r = 0; r < 4; ++r) o[t][r] = fmaf(o[t][r], alpha, x[r]);
+    }
   }
 }
 
@@ -295,11 +307,11 @@ struct PagedTile {
     }
     m = mn;
     l = l * alpha + sum;
-#pragma unroll
-    for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
     if (!paged_odd<T, D>(vw)) {
-      paged_values<T, D>(vw, p, o);
+      paged_values<T, D>(vw, p, alpha, o);
     } else {
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
       for (int32_t i = first / r.group; i < r.n_new && i * r.group < first + 16; ++i)
         paged_values_of<T, D>(vw, p, there ? r.sees(jl, r.len + i, r.len + i) : 0u, pos == r.len + i, o);
     }
