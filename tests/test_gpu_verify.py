@@ -172,6 +172,23 @@ def test_a_value_of_more_tokens_than_its_counter_holds():
             check(target, draft, torch.full((batch, 1), x, dtype=torch.int32, device="cuda"), None, ut[:, None].contiguous(), ut, params)
 
 
+def test_zeros_of_both_signs():
+    """Zeros of both signs are one value: the largest one, a middle one, or nothing above -inf but them."""
+    batch, vocab = 6, 20011                      # some of a row's first, inner and last parts
+    g = torch.Generator(device="cuda").manual_seed(14)
+    zero = torch.where(torch.rand((batch, 2, vocab), generator=g, device="cuda") < 0.5, 0.0, -0.0)
+    pick = torch.rand((batch, 2, vocab), generator=g, device="cuda")
+    target = torch.where(pick < 0.5, zero, torch.where(pick < 0.99, -1.0, 1.5)).bfloat16()
+    target[0] = torch.where(pick[0] < 0.5, zero[0], -0.5)
+    target[1], target[2] = -0.0, torch.where(pick[2] < 0.1, -0.0, -float("inf"))
+    draft = torch.where(pick[:, 1:] < 0.7, -zero[:, :1], 0.25).bfloat16()
+    params = [dict(top_k=4000), dict(top_p=0.4), dict(top_k=1500), dict(top_k=7001), dict(top_p=0.6), dict(min_p=0.1, top_p=0.8)]
+    for u in (0.07, 0.61):
+        ut = torch.full((batch,), u, device="cuda")
+        for x in (0, 9000):
+            check(target, draft, torch.full((batch, 1), x, dtype=torch.int32, device="cuda"), None, ut[:, None].contiguous(), ut, params)
+
+
 def test_tokens_are_distributed_as_the_target():
     """Over 512 x 40 draws the first token's frequencies are p's within five deviations."""
     g = torch.Generator(device="cuda").manual_seed(8)
