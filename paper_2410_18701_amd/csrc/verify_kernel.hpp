@@ -384,39 +384,9 @@ __global__ void __launch_bounds__(kSampleThreads) verify_rows_kernel(const Verif
   static_assert(!kValues || sizeof(ValueShared) <= sizeof(SampleShared) + kSampleRowBytes, "either fits");
   extern __shared__ __attribute__((aligned(16))) u32x4 lds[];
   SampleShared& s = *reinterpret_cast<SampleShared*>(lds);
-  // The slots whose rows take long first (fp32, 256 rows of 128,000: top_p 78 us, min_p 30 to
-  // 70, the others up to 25), so that the last ones are short.
-  const int32_t rank = blockIdx.x / a.slot_rows;
-  {
-    const int32_t b = threadIdx.x;
-    int32_t cost = -1;
-    if (b < a.batch) {
-      const int32_t top_k = a.top_k ? a.top_k[b] : 0;
-      const float top_p = a.top_p ? a.top_p[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f;
-      cost = top_k > 0 && top_k <= kSampleTopKList ? 0 : top_p < 1.f ? 2 : min_p > 0.f ? 1 : 0;
-    }
-    const uint64_t m2 = __ballot(cost == 2), m1 = __ballot(cost == 1), m0 = __ballot(cost == 0);
-    const int lane = b % kWave, w = b / kWave;
-    uint32_t* const n = s.count;           // per wave, of each cost
-    if (lane == 0) {
-      n[w] = __popcll(m2);
-      n[kSampleWaves + w] = __popcll(m1);
-      n[2 * kSampleWaves + w] = __popcll(m0);
-    }
-    __syncthreads();
-    if (cost >= 0) {
-      const int c = 2 - cost;
-      int32_t at = __popcll((cost == 2 ? m2 : cost == 1 ? m1 : m0) & ((1ull << lane) - 1));
-      for (int v = 0; v < c * kSampleWaves + w; ++v) at += n[v];
-      if (at == rank) s.found = b;
-    }
-    __syncthreads();
-  }
-  const int32_t slot = s.found;
   VerifyLogits l;
-  if (!l.find<T>(a, slot, blockIdx.x % a.slot_rows)) return;
+  if (!l.find<T>(a, blockIdx.x / a.slot_rows, blockIdx.x % a.slot_rows)) return;
   const int32_t r = l.r;
-  __syncthreads();                          // what is shared is free
   if (!l.pieces) {
     if constexpr (kValues) {
       if (verify_values_row(*reinterpret_cast<ValueShared*>(lds), l, a.kept + r)) return;
