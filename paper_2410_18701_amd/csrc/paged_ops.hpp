@@ -19,9 +19,20 @@ namespace baton {
 
 constexpr int kPagedBlock = 32;          // tokens per block
 constexpr int kPagedMaxNew = 16;         // == BATON_PAGED_MAX_WIDTH
-constexpr int kPagedItems = 2048;        // workgroups of an attention launch, about
-constexpr int kPagedRowItems = 512;      // and with more than 16 rows per head, which two a compute unit fill
-constexpr int kPagedMinBlocks = 8;       // blocks per work item, at least
+// Workgroups of an attention launch, about, and blocks per work item, at least.  Two
+// workgroups fit a compute unit, 512 the GPU.
+//  * Up to 16 rows per head, 2048: four rounds even out lengths, and every item costs its
+//    start and its part of the second launch.  With 1024, 2048 and 4096 a step of 32 slots
+//    of up to 2,048 tokens (32/32 heads) took 113, 105 and 102 us, two layers of 64 slots of
+//    up to 8,192 (64/8 heads) 399, 400 and 411.
+//  * More rows, 512: an item's start (its loads into LDS, its merge) is longer.  32 slots
+//    of very different lengths up to 32,768 (32/4 heads) with four drafts each: 84 us with
+//    256, 61 with 512, 65 with 1024.
+//  * 8 blocks, two a wave.  With 4, 8 and 16 a step of four slots of up to 128 tokens took
+//    14.3, 11.1 and 10.5 us, one of seven in fp32 with a window of 333 12.7, 12.9 and 16.8.
+constexpr int kPagedItems = 2048;
+constexpr int kPagedRowItems = 512;      // more than 16 rows
+constexpr int kPagedMinBlocks = 8;
 
 // A work item, one of a slot's `parts`: visible blocks v0 .. v1 - 1 of slot b.
 // Visible block v is the query's block v (v < sink) or v + skip.
@@ -100,8 +111,9 @@ __device__ __forceinline__ int32_t step_find(const int32_t* first, int32_t n, in
 // Ends a step and begins the next: lengths, pages given back and taken, places of the
 // new tokens, attention's work items.  One workgroup, a thread per slot for the sums
 // and all threads over the pages, places and items.  Pages are handed out in the order
-// of (slot, block) whatever order the threads run in.  Bound by the latency of its few
-// dependent reads and barriers.
+// of (slot, block) whatever order the threads run in.  One workgroup, as every number
+// depends on the sums over all slots; bound by the latency of its few dependent reads and
+// barriers: 4.2 us for one slot, 4.9 for 256 (a launch that does nothing: 3.4).
 __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedStepArgs a) {
   __shared__ uint64_t sums[3][kStepThreads / kWave];
   __shared__ int32_t first_back[kStepThreads + 1], first_more[kStepThreads + 1], first_item[kStepThreads + 1];
@@ -271,7 +283,8 @@ struct PagedCopyArgs {
 
 // One wave per block of 32 tokens of a layer, head, and K or V: through LDS, where the
 // values are transposed, so that memory sees whole rows on one side and whole chunks on
-// the other.  OUT: pages to queries.  Tokens behind the query's last are zeros.
+// the other.  Bound by memory: eight queries of up to 4,096 tokens 5.1 to 5.7 TB/s, read and
+// written (112 us in, 101 out; a plain copy 4.9).  OUT: pages to queries.  Tokens behind the query's last are zeros.
 template <int ES, int D, bool OUT>
 __global__ void __launch_bounds__(kWave) paged_copy_kernel(const PagedCopyArgs a) {
   constexpr int ROW = D * ES, VECS = 32 * ROW / 1024, CH = ROW / 64, LDR = ROW + 16;
