@@ -61,35 +61,6 @@ struct PagedGeo {
   typedef u32x4 Vecs[kVecs];                        // a lane's part of a block's K, or V
 };
 
-// Keys and values of the step's new tokens that lie in this block, from their rows into
-// the pages.  The wave that stores them reads the block back itself.
-template <typename T, int D>
-__device__ __forceinline__ void paged_append(const PagedAttnArgs& a, const PagedItem& it, int32_t h, int32_t block,
-                                             uint8_t* kb, uint8_t* vb, int lane) {
-  using Geo = PagedGeo<T, D>;
-  constexpr int P = Geo::kRow / 16;
-  const int32_t j0 = max(it.len, block * kPagedBlock), n = min(it.len + it.n_new, (block + 1) * kPagedBlock) - j0;
-  const int64_t row0 = (((int64_t)it.b * a.width + (j0 - it.len)) * a.n_kv_heads + h) * Geo::kRow;
-  const int64_t step = (int64_t)a.n_kv_heads * Geo::kRow;       // from token to token
-#pragma unroll 4
-  for (int32_t idx = lane; idx < n * P; idx += kWave) {
-    const int32_t j = idx / P, p = idx % P, t = (j0 + j) % kPagedBlock;
-    const u32x4 w = *reinterpret_cast<const u32x4*>(a.k_new + row0 + j * step + p * 16);
-    *reinterpret_cast<u32x4*>(kb + ((((t >> 2 & 1) * Geo::kChunks + p / 4) * 64) + (p % 4) * 16 + 4 * (t >> 3) + (t & 3)) * 16) = w;
-  }
-#pragma unroll 4
-  for (int32_t idx = lane; idx < n * D; idx += kWave) {
-    const int32_t j = idx / D, d = idx % D, t = (j0 + j) % kPagedBlock;
-    if constexpr (T::kBytes == 2)
-      *reinterpret_cast<uint16_t*>(vb + ((d / 16 * 64) + (t >> 3) * 16 + d % 16) * 16 + (t & 7) * 2) =
-          reinterpret_cast<const uint16_t*>(a.v_new + row0 + j * step)[d];
-    else
-      *reinterpret_cast<uint32_t*>(vb + ((((t >> 2) & 1) * Geo::kDt + d / 16) * 64 + (t >> 3) * 16 + d % 16) * 16 + (t & 3) * 4) =
-          reinterpret_cast<const uint32_t*>(a.v_new + row0 + j * step)[d];
-  }
-  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the stores are done before the block is read
-}
-
 // Scores of 32 tokens against 16 rows: s[e] for token 8 (lane / 16) + e of row lane % 16.
 // fp32: four sums per score, so that each has fewer roundings (and waits for fewer of its
 // own products).
@@ -408,6 +379,52 @@ __device__ __forceinline__ int32_t paged_block_of(const PagedItem& it, int32_t k
   const int32_t v = it.v0 + k;
   return v < it.sink ? v : v + it.skip;
 }
+// Keys and values of the step's new tokens that lie in this block -- of them, every BY-th
+// from `from` on --, from their rows into the pages, if the block has one.  All loads at
+// once, before the page's number is waited for: with runs of V's elements, waited for one
+// after the other by one wave, an item's start took 5 to 12 us (32 slots with four drafts,
+// lengths up to 32,768: a step 61.5 us, with all loads at once 60.9, all waves 58.2).
+template <typename T, int D, int BY>
+__device__ __forceinline__ void paged_append(const PagedAttnArgs& a, const PagedItem& it, int32_t h, int32_t block,
+                                             int32_t shift, int32_t from, int lane) {
+  using Geo = PagedGeo<T, D>;
+  constexpr int P = Geo::kRow / 16, NI = (kPagedMaxNew / BY * P + kWave - 1) / kWave;
+  const int32_t j0 = max(it.len, block * kPagedBlock), n = min(it.len + it.n_new, (block + 1) * kPagedBlock) - j0;
+  const int64_t row0 = (((int64_t)it.b * a.width + (j0 - it.len)) * a.n_kv_heads + h) * Geo::kRow;
+  const int64_t step = (int64_t)a.n_kv_heads * Geo::kRow;       // from token to token
+  const int32_t page = paged_page(a, it, block, shift);
+  u32x4 kw[NI], vw[NI];
+#pragma unroll
+  for (int u = 0; u < NI; ++u) {
+    const int32_t idx = u * kWave + lane, j = from + idx / P * BY;
+    if (j >= n) continue;
+    const int64_t at = row0 + j * step + idx % P * 16;
+    kw[u] = *reinterpret_cast<const u32x4*>(a.k_new + at);
+    vw[u] = *reinterpret_cast<const u32x4*>(a.v_new + at);
+  }
+  const int32_t id = __builtin_amdgcn_readfirstlane(page);
+  if (id < 0) return;
+  const int64_t off = paged_offset<T, D>(a, id, h, block, shift);
+  uint8_t* const kb = a.k + off;
+  uint8_t* const vb = a.v + off;
+#pragma unroll
+  for (int u = 0; u < NI; ++u) {
+    const int32_t idx = u * kWave + lane, p = idx % P, j = from + idx / P * BY, t = (j0 + j) % kPagedBlock;
+    if (j >= n) continue;
+    *reinterpret_cast<u32x4*>(kb + ((((t >> 2 & 1) * Geo::kChunks + p / 4) * 64) + (p % 4) * 16 + 4 * (t >> 3) + (t & 3)) * 16) = kw[u];
+    if constexpr (T::kBytes == 2) {
+      uint8_t* const to = vb + (p / 2 * 64 + (t >> 3) * 16 + p % 2 * 8) * 16 + (t & 7) * 2;     // columns 8 p ..
+#pragma unroll
+      for (int e = 0; e < 8; ++e) *reinterpret_cast<uint16_t*>(to + e * 16) = (uint16_t)(vw[u][e / 2] >> (16 * (e % 2)));
+    } else {
+      uint8_t* const to = vb + (((t >> 2 & 1) * Geo::kDt + p / 4) * 64 + (t >> 3) * 16 + p % 4 * 4) * 16 + (t & 3) * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(to + e * 16) = vw[u][e];         // columns 4 p ..
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // the stores are done before the block is read
+}
+
 // 16 bytes of row r's query.
 template <typename T, int D>
 __device__ __forceinline__ u32x4 paged_query(const PagedAttnArgs& a, const PagedItem& it, int32_t h, int32_t r, int c, int g4) {
@@ -451,12 +468,8 @@ paged_attn_kernel(const PagedAttnArgs a) {
 #pragma unroll
   for (int c = 0; c < CH; ++c) qw[c] = paged_query<T, D>(a, it, h, c16, c, g4);
   if (a.k_new) {       // the new tokens of its blocks (the last ones) first
-    for (int32_t k = n_mine - 1; k >= 0 && block_of(k) * kPagedBlock + kPagedBlock > it.len; --k) {
-      const int32_t block = block_of(k), id = __builtin_amdgcn_readfirstlane(paged_page(a, it, block, r.shift));
-      if (id < 0) continue;
-      const int64_t off = paged_offset<T, D>(a, id, h, block, r.shift);
-      paged_append<T, D>(a, it, h, block, a.k + off, a.v + off, lane);
-    }
+    for (int32_t k = n_mine - 1; k >= 0 && block_of(k) * kPagedBlock + kPagedBlock > it.len; --k)
+      paged_append<T, D, 1>(a, it, h, block_of(k), r.shift, 0, lane);
   }
   PagedTile<D> x(r, 0, c16);
 
@@ -520,13 +533,14 @@ __device__ __forceinline__ void paged_load_lds(const uint8_t* from, uint32_t l16
 // Up to 64 rows.  Blocks go from memory into LDS, without registers, some blocks ahead, and
 // the waves share them: with more than 32 rows each wave has a tile of its own, with 32 two
 // waves share a tile and take turns at the blocks, with 16 all four do.  32 slots with
-// four drafts each (32/4 heads, lengths up to 32,768, most far shorter): 53 us; a step in which every wave took
-// four tiles after one another, from its own registers, was 92 instead of 63.  Bound by the waves' own chain of
-// products, maxima and exponentials (waiting 64% of their cycles; 29% of the matrix cores'),
-// as two workgroups' LDS fills a compute unit: the bytes alone would take 32.  A call's
-// largest possible number of rows decides between the kernels: for up to 16 this one took
-// 131 us instead of 105 (32 slots of up to 2,048 tokens, 32/32 heads) and 470 instead of
-// 400 (two layers of 64 of up to 8,192, 64/8 heads).
+// four drafts each (32/4 heads, lengths up to 32,768, most far shorter): 50 us, where the
+// bytes alone take 32; a step in which every wave took four tiles after one another, from
+// its own registers, was 92 instead of 63.  The loop over an item's blocks takes the same
+// with 8 rows as with 40: it is bound by the blocks on their way, three for each of the two
+// workgroups whose LDS fills a compute unit, 14 bytes a nanosecond for one workgroup and 21
+// for two.  A call's largest possible number of rows decides between the kernels: for up to
+// 16 this one took 131 us instead of 105 (32 slots of up to 2,048 tokens, 32/32 heads) and
+// 470 instead of 400 (two layers of 64 of up to 8,192, 64/8 heads).
 template <typename T, int D>
 __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_rows_kernel(const PagedAttnArgs a) {
   using Geo = PagedGeo<T, D>;
@@ -551,13 +565,9 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_rows_kernel(co
   u32x4 qw[CH];
 #pragma unroll
   for (int c = 0; c < CH; ++c) qw[c] = paged_query<T, D>(a, it, h, tile * 16 + c16, c, g4);
-  if (a.k_new) {       // the new tokens of the item's blocks (the last ones) first, a wave a block
-    for (int32_t k = n - 1; k >= 0 && paged_block_of(it, k) * kPagedBlock + kPagedBlock > it.len; --k) {
-      const int32_t block = paged_block_of(it, k), id = __builtin_amdgcn_readfirstlane(paged_page(a, it, block, r.shift));
-      if (id < 0 || k % kPagedWaves != w) continue;
-      const int64_t off = paged_offset<T, D>(a, id, h, block, r.shift);
-      paged_append<T, D>(a, it, h, block, a.k + off, a.v + off, lane);
-    }
+  if (a.k_new) {       // the new tokens of the item's blocks (the last ones) first, by all waves
+    for (int32_t k = n - 1; k >= 0 && paged_block_of(it, k) * kPagedBlock + kPagedBlock > it.len; --k)
+      paged_append<T, D, kPagedWaves>(a, it, h, paged_block_of(it, k), r.shift, w, lane);
     __syncthreads();
   }
   PagedTile<D> x(r, tile, c16);
