@@ -508,13 +508,11 @@ paged_attn_kernel(const PagedAttnArgs a) {
   if (w == 0) paged_write<T, D>(a, it, item, h, x, lane);
 }
 
-// This wave's LDS reads and all but its last VM vector loads are done, then the barrier:
-// __syncthreads() does not promise that another wave's loads into LDS have landed.
-template <int VM>
+// This wave's LDS reads and vector loads are done, then the barrier: __syncthreads() does not
+// promise that another wave's loads into LDS have landed.
 __device__ __forceinline__ void paged_wait_and_barrier() {
-  static_assert(VM < 16, "vmcnt's low four bits");
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070 | VM);       // vmcnt <= VM, lgkmcnt 0
+  __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt 0, lgkmcnt 0
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -530,27 +528,23 @@ __device__ __forceinline__ void paged_load_lds(const uint8_t* from, uint32_t l16
 #endif
 }
 
-// Up to 64 rows.  Blocks go from memory into LDS, without registers, some blocks ahead, and
-// the waves share them: with more than 32 rows each wave has a tile of its own, with 32 two
-// waves share a tile and take turns at the blocks, with 16 all four do.  32 slots with
-// four drafts each (32/4 heads, lengths up to 32,768, most far shorter): 50 us, where the
-// bytes alone take 32; a step in which every wave took four tiles after one another, from
-// its own registers, was 92 instead of 63.  The loop over an item's blocks takes the same
-// with 8 rows as with 40: it is bound by the blocks on their way, three for each of the two
-// workgroups whose LDS fills a compute unit, 14 bytes a nanosecond for one workgroup and 21
-// for two.  A call's largest possible number of rows decides between the kernels: for up to
-// 16 this one took 131 us instead of 105 (32 slots of up to 2,048 tokens, 32/32 heads) and
-// 470 instead of 400 (two layers of 64 of up to 8,192, 64/8 heads).
+// Up to 64 rows.  Blocks go from memory into LDS, without registers, a pair of them while the
+// last pair is worked on, and the waves share them: with more than 32 rows each wave has a
+// tile of its own, with 32 two waves share a tile and a pair, with 16 two waves at a time have
+// a block.  32 slots with four drafts each (32/4 heads, lengths up to 32,768, most far
+// shorter): 52 us a step, whose bytes take 32.  Waves wait for loads 3% of the loop; it is
+// bound by a tile's chain of product, maximum, exponential and product, some 2,800 cycles a
+// block with a barrier at each (58 us, three blocks ahead; 56 with two), which a pair's
+// two chains overlap.  A call's largest possible number of rows decides between the kernels:
+// for up to 16 this one, with a barrier a block, took 131 us instead of 105 (32 slots of up to
+// 2,048 tokens, 32/32 heads) and 470 instead of 400 (two layers of 64 of up to 8,192, 64/8).
 template <typename T, int D>
-__global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_rows_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(kWave * kPagedWaves) __attribute__((amdgpu_waves_per_eu(T::kBytes == 4 && D == 128 ? 1 : 2)))
+paged_attn_rows_kernel(const PagedAttnArgs a) {
   using Geo = PagedGeo<T, D>;
   constexpr int CH = Geo::kChunks, NV = Geo::kVecs;
-  constexpr int BB = 2 * NV * 1024;              // bytes of a block's K and V
-  constexpr int R = BB <= 16384 ? 4 : 3;         // blocks in LDS
   constexpr int NL = 2 * NV / kPagedWaves;       // loads per wave and block
-  // a buffer each, not an array: reads of one must not wait for the loads into another
-  __shared__ __attribute__((aligned(1024))) u32x4 buf0[2 * NV][kWave], buf1[2 * NV][kWave], buf2[2 * NV][kWave];
-  __shared__ __attribute__((aligned(1024))) u32x4 buf3[R == 4 ? 2 * NV : 1][kWave];
+  __shared__ __attribute__((aligned(1024))) u32x4 ring[4][2 * NV][kWave];     // two pairs of blocks, K and V of each
   __shared__ float sm_m[kPagedWaves][16], sm_l[kPagedWaves][16];
   const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
   const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];   // (the list has room for all)
@@ -578,8 +572,7 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_rows_kernel(co
     const int32_t ids = lane < nk ? paged_page(a, it, paged_block_of(it, k0 + lane), r.shift) : -1;
     paged_wait_loads();
     int32_t fetched = 0;
-    // The next block into LDS, a fourth of it by this wave (past the last one: that one
-    // again, so that the number of loads on their way is always the same).
+    // The next block into LDS, a fourth of it by this wave (past the last one: that one again).
     auto fetch = [&](u32x4 (*to)[kWave]) {
       const int32_t k = min(fetched, nk - 1), id = __builtin_amdgcn_readlane(ids, k);
       const int64_t off = paged_offset<T, D>(a, max(id, 0), h, paged_block_of(it, k0 + k), r.shift);
@@ -590,51 +583,51 @@ __global__ void __launch_bounds__(kWave * kPagedWaves) paged_attn_rows_kernel(co
       }
       ++fetched;
     };
-    // Block k from its buffer.  The barrier comes after every load but those of the R - 2
-    // blocks behind it, and after every wave's reads of block k - 1, whose buffer is free then.
-    auto step = [&](int32_t k, u32x4 (*from)[kWave], u32x4 (*free)[kWave]) {
-      paged_wait_and_barrier<NL * (R - 2)>();
-      fetch(free);
-      if ((k0 + k) % groups != turn || tile * 16 >= rows) return;
-      float s[8];
-      {
+    fetch(ring[0]);
+    fetch(ring[1]);
+    for (int32_t k = 0; k < nk; k += 2) {
+      const u32x4 (*const pair)[2 * NV][kWave] = ring + (k & 2);
+      // The pair has landed, and every wave is done with the other two buffers.
+      paged_wait_and_barrier();
+      if (k + 2 < nk) {
+        fetch(ring[2 - (k & 2)]);
+        fetch(ring[3 - (k & 2)]);
+      }
+      if (tile * 16 >= rows) continue;
+      const bool first = (k0 + k) % groups == turn, second = k + 1 < nk && (k0 + k + 1) % groups == turn;
+      auto scores = [&](int q, float (&s)[8]) {
         typename Geo::Vecs kw;
 #pragma unroll
-        for (int u = 0; u < NV; ++u) kw[u] = from[u][lane];
+        for (int u = 0; u < NV; ++u) kw[u] = pair[q][u][lane];
         paged_scores<T, D>(kw, qw, s);
-      }
-      typename Geo::Vecs vw;
+      };
+      auto values = [&](int q, typename Geo::Vecs& vw) {
 #pragma unroll
-      for (int u = 0; u < NV; ++u) vw[u] = from[NV + u][lane];
-      x.template add<T>(r, paged_block_of(it, k0 + k) * kPagedBlock, __builtin_amdgcn_readlane(ids, k) >= 0, s, vw, g4);
-    };
-    fetch(buf0);
-    fetch(buf1);
-    if constexpr (R == 4) {
-      fetch(buf2);
-      for (int32_t k = 0;; k += 4) {
-        step(k, buf0, buf3);
-        if (k + 1 >= nk) break;
-        step(k + 1, buf1, buf0);
-        if (k + 2 >= nk) break;
-        step(k + 2, buf2, buf1);
-        if (k + 3 >= nk) break;
-        step(k + 3, buf3, buf2);
-        if (k + 4 >= nk) break;
-      }
-    } else {
-      for (int32_t k = 0;; k += 3) {
-        step(k, buf0, buf2);
-        if (k + 1 >= nk) break;
-        step(k + 1, buf1, buf0);
-        if (k + 2 >= nk) break;
-        step(k + 2, buf2, buf1);
-        if (k + 3 >= nk) break;
+        for (int u = 0; u < NV; ++u) vw[u] = pair[q][NV + u][lane];
+      };
+      auto add = [&](int q, float (&s)[8], typename Geo::Vecs& vw) {
+        x.template add<T>(r, paged_block_of(it, k0 + k + q) * kPagedBlock, __builtin_amdgcn_readlane(ids, k + q) >= 0, s, vw, g4);
+      };
+      float s[8];
+      typename Geo::Vecs vw;
+      if (first && second) {
+        float s2[8];
+        typename Geo::Vecs vw2;
+        scores(0, s);
+        scores(1, s2);
+        values(0, vw);
+        values(1, vw2);
+        add(0, s, vw);
+        add(1, s2, vw2);
+      } else if (first || second) {
+        scores(second, s);
+        values(second, vw);
+        add(second, s, vw);
       }
     }
-    paged_wait_and_barrier<0>();                    // no load is on its way into what is used next
+    paged_wait_and_barrier();                    // every wave is done with the buffers
   }
-  paged_merge<D>(x, groups, buf0, sm_m, sm_l, w, lane);
+  paged_merge<D>(x, groups, ring[0], sm_m, sm_l, w, lane);
   if (turn == 0) paged_write<T, D>(a, it, item, h, x, lane);
 }
 
