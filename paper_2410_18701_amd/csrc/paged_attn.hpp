@@ -223,6 +223,10 @@ struct PagedRows {
   int32_t len, n_new, group, window, sinks, shift;   // shift: log2 of a page's blocks
   float qscale, qscale_rest;
 
+  __device__ __forceinline__ PagedRows(const PagedAttnArgs& a, const PagedItem& it)
+      : len(it.len), n_new(it.n_new), group(a.group), window(a.window), sinks(a.sinks), shift(a.page_shift - 5),
+        qscale(a.qscale), qscale_rest(a.qscale_rest) {}
+
   // Bit e: a token at a position from p0 to p1 sees token j + e.
   __device__ __forceinline__ uint32_t sees(int32_t j, int32_t p0, int32_t p1) const {
     uint32_t bits = 0;
@@ -438,29 +442,16 @@ __device__ __forceinline__ u32x4 paged_query(const PagedAttnArgs& a, const Paged
 // lanes without a block take; told so, the compiler does not wait in the loops behind it.
 __device__ __forceinline__ void paged_wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
-// Up to 16 rows.  Every wave has all of them, and every fourth of the item's blocks, whose
-// keys and values go from memory into its registers: 1 KB of consecutive bytes per load, no
-// LDS and no barrier until the merge.  Bound by memory: 64 slots of up to 8,192 tokens (64/8
-// heads, bf16) take 193 us a layer, 5.9 TB/s of 6.09 that a plain read of that size reaches;
-// 32 of up to 2,048 (32/32 heads) 99 us, 5.8 TB/s.  The matrix cores are busy a quarter of
-// the time.  Two waves a SIMD are asked for (fp32 at head_dim 128, whose blocks are twice as
-// large: one), which leaves registers for K and V of a block each; with all of a SIMD's
-// registers for one wave the steps took 423 us instead of 405 (two layers), 119 instead of
-// 105.
+// An item of up to 16 rows.  Every wave has all of them, and every fourth of the item's
+// blocks, whose keys and values go from memory into its registers: 1 KB of consecutive bytes
+// per load, no LDS and no barrier until the merge.
 template <typename T, int D>
-__global__ void __launch_bounds__(kWave * kPagedWaves) __attribute__((amdgpu_waves_per_eu(T::kBytes == 4 && D == 128 ? 1 : 2)))
-paged_attn_kernel(const PagedAttnArgs a) {
+__device__ __forceinline__ void paged_item16(const PagedAttnArgs& a, const PagedItem& it, int32_t item, int32_t h,
+                                             const PagedRows& r, u32x4 (*sm)[kWave], float (*sm_m)[16], float (*sm_l)[16]) {
   using Geo = PagedGeo<T, D>;
   constexpr int CH = Geo::kChunks, NV = Geo::kVecs;
-  __shared__ u32x4 sm[kPagedWaves / 2 * Geo::kDt][kWave];
-  __shared__ float sm_m[kPagedWaves][16], sm_l[kPagedWaves][16];
-  const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
-  const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];   // (the list has room for all)
-  if (item >= a.state[kNumItems] || it.n_new > a.width) return;   // the latter: more than the call brings
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int g4 = lane / 16, c16 = lane % 16;
-  const PagedRows r = {it.len, it.n_new, a.group, a.window, a.sinks, a.page_shift - 5, a.qscale, a.qscale_rest};
-
   // This wave's blocks: w, w + 4, ... of the item.
   const int32_t n_mine = (it.v1 - it.v0 - w + kPagedWaves - 1) / kPagedWaves;
   auto block_of = [&](int32_t k) { return paged_block_of(it, w + k * kPagedWaves); };
@@ -508,6 +499,25 @@ paged_attn_kernel(const PagedAttnArgs a) {
   if (w == 0) paged_write<T, D>(a, it, item, h, x, lane);
 }
 
+// Calls of up to 16 rows. Bound by memory: 64 slots of up to 8,192 tokens (64/8
+// heads, bf16) take 193 us a layer, 5.9 TB/s of 6.09 that a plain read of that size reaches;
+// 32 of up to 2,048 (32/32 heads) 99 us, 5.8 TB/s.  The matrix cores are busy a quarter of
+// the time.  Two waves a SIMD are asked for (fp32 at head_dim 128, whose blocks are twice as
+// large: one), which leaves registers for K and V of a block each; with all of a SIMD's
+// registers for one wave the steps took 423 us instead of 405 (two layers), 119 instead of
+// 105.
+template <typename T, int D>
+__global__ void __launch_bounds__(kWave * kPagedWaves) __attribute__((amdgpu_waves_per_eu(T::kBytes == 4 && D == 128 ? 1 : 2)))
+paged_attn_kernel(const PagedAttnArgs a) {
+  using Geo = PagedGeo<T, D>;
+  __shared__ u32x4 sm[kPagedWaves / 2 * Geo::kDt][kWave];
+  __shared__ float sm_m[kPagedWaves][16], sm_l[kPagedWaves][16];
+  const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
+  const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];   // (the list has room for all)
+  if (item >= a.state[kNumItems] || it.n_new > a.width) return;   // the latter: more than the call brings
+  paged_item16<T, D>(a, it, item, h, PagedRows(a, it), sm, sm_m, sm_l);
+}
+
 // This wave's LDS reads and vector loads are done, then the barrier: __syncthreads() does not
 // promise that another wave's loads into LDS have landed.
 __device__ __forceinline__ void paged_wait_and_barrier() {
@@ -551,9 +561,13 @@ paged_attn_rows_kernel(const PagedAttnArgs a) {
   if (item >= a.state[kNumItems] || it.n_new > a.width) return;   // the latter: more than the call brings
   const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int g4 = lane / 16, c16 = lane % 16;
-  const PagedRows r = {it.len, it.n_new, a.group, a.window, a.sinks, a.page_shift - 5, a.qscale, a.qscale_rest};
+  const PagedRows r(a, it);
   const int32_t n = it.v1 - it.v0, rows = it.n_new * a.group;
-  const int32_t tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, groups = kPagedWaves / tiles;
+  if (rows <= 16) {
+    paged_item16<T, D>(a, it, item, h, r, ring[0], sm_m, sm_l);
+    return;
+  }
+  const int32_t tiles = rows <= 32 ? 2 : 4, groups = kPagedWaves / tiles;
   const int32_t tile = w % tiles, turn = w / tiles;
 
   u32x4 qw[CH];
