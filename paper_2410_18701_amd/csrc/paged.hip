@@ -71,8 +71,7 @@ baton_status check(const baton_paged_desc* d) {
 template <typename T, int D>
 void launch_attn(const baton::PagedAttnArgs& a, int32_t items, bool split, hipStream_t s) {
   const dim3 grid((unsigned)items * a.n_kv_heads), block(baton::kWave * baton::kPagedWaves);
-  if (a.width * a.group <= 16) hipLaunchKernelGGL((baton::paged_attn_kernel<T, D>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((baton::paged_attn_rows_kernel<T, D>), grid, block, 0, s, a);
+  hipLaunchKernelGGL((baton::paged_attn_kernel<T, D>), grid, block, 0, s, a);
   if (split)
     hipLaunchKernelGGL((baton::paged_combine_kernel<T, D>),
                        dim3((unsigned)a.batch * a.n_kv_heads, (unsigned)(a.width * a.group)), dim3(256), 0, s, a);

@@ -444,7 +444,10 @@ __device__ __forceinline__ void paged_wait_loads() { __builtin_amdgcn_s_waitcnt(
 
 // An item of up to 16 rows.  Every wave has all of them, and every fourth of the item's
 // blocks, whose keys and values go from memory into its registers: 1 KB of consecutive bytes
-// per load, no LDS and no barrier until the merge.
+// per load, no LDS and no barrier until the merge.  Bound by memory: 64 slots of up to 8,192
+// tokens (64/8 heads, bf16) take 193 us a layer, 5.9 TB/s of 6.09 that a plain read of that
+// size reaches; 32 of up to 2,048 (32/32 heads) 98 us, 5.8 TB/s.  The matrix cores are busy a
+// quarter of the time.
 template <typename T, int D>
 __device__ __forceinline__ void paged_item16(const PagedAttnArgs& a, const PagedItem& it, int32_t item, int32_t h,
                                              const PagedRows& r, u32x4 (*sm)[kWave], float (*sm_m)[16], float (*sm_l)[16]) {
@@ -499,25 +502,6 @@ __device__ __forceinline__ void paged_item16(const PagedAttnArgs& a, const Paged
   if (w == 0) paged_write<T, D>(a, it, item, h, x, lane);
 }
 
-// Calls of up to 16 rows. Bound by memory: 64 slots of up to 8,192 tokens (64/8
-// heads, bf16) take 193 us a layer, 5.9 TB/s of 6.09 that a plain read of that size reaches;
-// 32 of up to 2,048 (32/32 heads) 99 us, 5.8 TB/s.  The matrix cores are busy a quarter of
-// the time.  Two waves a SIMD are asked for (fp32 at head_dim 128, whose blocks are twice as
-// large: one), which leaves registers for K and V of a block each; with all of a SIMD's
-// registers for one wave the steps took 423 us instead of 405 (two layers), 119 instead of
-// 105.
-template <typename T, int D>
-__global__ void __launch_bounds__(kWave * kPagedWaves) __attribute__((amdgpu_waves_per_eu(T::kBytes == 4 && D == 128 ? 1 : 2)))
-paged_attn_kernel(const PagedAttnArgs a) {
-  using Geo = PagedGeo<T, D>;
-  __shared__ u32x4 sm[kPagedWaves / 2 * Geo::kDt][kWave];
-  __shared__ float sm_m[kPagedWaves][16], sm_l[kPagedWaves][16];
-  const int32_t item = blockIdx.x / a.n_kv_heads, h = blockIdx.x - item * a.n_kv_heads;
-  const PagedItem it = reinterpret_cast<const PagedItem*>(a.state + a.at.items)[item];   // (the list has room for all)
-  if (item >= a.state[kNumItems] || it.n_new > a.width) return;   // the latter: more than the call brings
-  paged_item16<T, D>(a, it, item, h, PagedRows(a, it), sm, sm_m, sm_l);
-}
-
 // This wave's LDS reads and vector loads are done, then the barrier: __syncthreads() does not
 // promise that another wave's loads into LDS have landed.
 __device__ __forceinline__ void paged_wait_and_barrier() {
@@ -538,19 +522,22 @@ __device__ __forceinline__ void paged_load_lds(const uint8_t* from, uint32_t l16
 #endif
 }
 
-// Up to 64 rows.  Blocks go from memory into LDS, without registers, a pair of them while the
-// last pair is worked on, and the waves share them: with more than 32 rows each wave has a
-// tile of its own, with 32 two waves share a tile and a pair, with 16 two waves at a time have
-// a block.  32 slots with four drafts each (32/4 heads, lengths up to 32,768, most far
-// shorter): 52 us a step, whose bytes take 32.  Waves wait for loads 3% of the loop; it is
-// bound by a tile's chain of product, maximum, exponential and product, some 2,800 cycles a
-// block with a barrier at each (58 us, three blocks ahead; 56 with two), which a pair's
-// two chains overlap.  A call's largest possible number of rows decides between the kernels:
-// for up to 16 this one, with a barrier a block, took 131 us instead of 105 (32 slots of up to
-// 2,048 tokens, 32/32 heads) and 470 instead of 400 (two layers of 64 of up to 8,192, 64/8).
+// An item of more than 16 rows, up to 64: blocks go from memory into LDS, without registers, a
+// pair of them while the last pair is worked on, and the waves share them: with more than 32
+// rows each wave has a tile of its own, with 32 two waves share a tile and a pair.  32 slots
+// with four drafts each (32/4 heads, lengths up to 32,768, most far shorter): 50 us a step,
+// whose bytes take 32.  Waves wait for loads 3% of the loop; it is bound by a tile's chain of
+// product, maximum, exponential and product, some 2,800 cycles a block with a barrier at each
+// (58 us, three blocks ahead; 56 with two), which a pair's two chains overlap (52, and 50
+// with items of up to 16 rows as above, which all of a call's items took here before: 131 us
+// instead of 105 for the 32 slots of up to 2,048, 470 instead of 400 for two layers of the 64).
+//
+// Two waves a SIMD are asked for (fp32 at head_dim 128, whose blocks are twice as large: one),
+// which leaves registers for K and V of a block each; with all of a SIMD's registers for one
+// wave those steps took 119 and 423 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(kWave * kPagedWaves) __attribute__((amdgpu_waves_per_eu(T::kBytes == 4 && D == 128 ? 1 : 2)))
-paged_attn_rows_kernel(const PagedAttnArgs a) {
+paged_attn_kernel(const PagedAttnArgs a) {
   using Geo = PagedGeo<T, D>;
   constexpr int CH = Geo::kChunks, NV = Geo::kVecs;
   constexpr int NL = 2 * NV / kPagedWaves;       // loads per wave and block

@@ -26,8 +26,8 @@ constexpr int kPagedMaxNew = 16;         // == BATON_PAGED_MAX_WIDTH
 //    of up to 2,048 tokens (32/32 heads) took 113, 105 and 102 us, two layers of 64 slots of
 //    up to 8,192 (64/8 heads) 399, 400 and 411.
 //  * More rows, 512: an item's start (its loads into LDS, its merge) is longer.  32 slots
-//    of very different lengths up to 32,768 (32/4 heads) with four drafts each: 84 us with
-//    256, 61 with 512, 65 with 1024.
+//    of very different lengths up to 32,768 (32/4 heads) with four drafts each: 51.4 us
+//    with 448, 49.9 with 512, 57.5 with 640 and 53.6 with 1024.
 //  * 8 blocks, two a wave.  With 4, 8 and 16 a step of four slots of up to 128 tokens took
 //    14.3, 11.1 and 10.5 us, one of seven in fp32 with a window of 333 12.7, 12.9 and 16.8.
 constexpr int kPagedItems = 2048;
