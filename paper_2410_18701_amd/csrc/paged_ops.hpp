@@ -13,7 +13,7 @@
 //    per column slice and tile holds the tile's.
 #pragma once
 
-#include "common.hpp"
+#include "wave_scan.hpp"
 
 namespace baton {
 

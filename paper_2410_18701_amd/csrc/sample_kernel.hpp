@@ -40,7 +40,7 @@
 // of which 13.5 is the first read and 33 the bins' weights.
 #pragma once
 
-#include "common.hpp"
+#include "wave_scan.hpp"
 
 namespace baton {
 namespace {
