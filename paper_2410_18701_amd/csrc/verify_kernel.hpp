@@ -19,7 +19,7 @@
 // order: the same inputs give the same tokens.
 //
 // Four launches (3.4 us each if they did nothing), 19 us for one slot of three drafts over
-// 50,257, fp32.  64 slots of four drafts over 128,000, bf16, parameters of all kinds: 24 + 73 + 20
+// 50,257, fp32.  64 slots of four drafts over 128,000, bf16, parameters of all kinds: 24 + 74 + 20
 // + 9 us, of which the first two read 118 MB (20 us at a plain read's rate).
 #pragma once
 
@@ -177,7 +177,8 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_pieces_kernel(const Ver
 // pass over the row, one weight for each value that is there, and a second pass for the
 // token's index.  480 rows of 128,000, two rounds of the GPU as the counters fill a compute
 // unit's LDS: top_p 105 us, top_k 81, min_p 83, where bins of weights take 192, 89 and 106.
-// Bound by latency: of a row's reads by one workgroup, and of the steps behind them.
+// A row: 16 us to be counted (all compute units together read 4.2 TB/s then), 11 for weights
+// and prefixes, 0 to 17 until the index is found.
 constexpr int kValueWords = 32768;       // two counters each
 
 struct ValueShared {
