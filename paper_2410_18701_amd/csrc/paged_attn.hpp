@@ -13,8 +13,8 @@
 //  * softmax with a running maximum per row, in fp32, base 2.
 //  * O^T += V^T P^T, where lane l supplies as it holds them its own row's weights, and
 //    accumulates columns 16 t + 4 (l / 16) .. + 3 of row l % 16.
-// bf16: weights are taken as a sum of two bf16 numbers, so that they have 16 bits for
-// their product with the values; the values' and keys' products are exact in fp32.
+// bf16: weights are taken as a sum of three bf16 numbers, which have all of fp32's bits;
+// the values' and keys' products with them are exact in fp32.
 // fp32: products in fp32 (v_mfma_f32_16x16x4_f32).
 // K and V come from memory in the order of the operands.
 // Values that are infinite or NaN: a weight of 0 would turn them into NaN for rows that
@@ -94,6 +94,28 @@ __device__ __forceinline__ void paged_scores(const typename PagedGeo<T, D>::Vecs
   }
 }
 
+// fp32 weights as three bf16 numbers each, of 8 bits: their sum is the weight.
+struct PagedWeights {
+  pa_bf16x8 part[3];
+
+  __device__ __forceinline__ explicit PagedWeights(const float (&p)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float rest = p[e];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        part[i][e] = (__bf16)rest;
+        rest -= (float)part[i][e];
+      }
+    }
+  }
+};
+
+// Pairs of bf16 numbers, infinite or NaN ones set to zero.
+__device__ __forceinline__ uint32_t paged_finite(uint32_t x) {
+  return x & (((x & 0x7F80u) != 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) != 0x7F800000u ? 0xFFFF0000u : 0u));
+}
+
 // o = alpha o + V^T P^T over 32 tokens, finite values.  fp32: the block's sum by itself, so
 // that a long row's has a rounding per block, not per product.
 template <typename T, int D>
@@ -101,18 +123,13 @@ __device__ __forceinline__ void paged_values(const typename PagedGeo<T, D>::Vecs
                                              float alpha, pa_f32x4 (&o)[D / 16]) {
   constexpr int DT = D / 16;
   if constexpr (T::kBytes == 2) {
-    pa_bf16x8 hi, lo;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      hi[e] = (__bf16)p[e];
-      lo[e] = (__bf16)(p[e] - (float)hi[e]);
-    }
+    const PagedWeights w(p);
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
       const pa_bf16x8 v = __builtin_bit_cast(pa_bf16x8, vw[t]);
       o[t] *= alpha;
-      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, o[t], 0, 0, 0);
-      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, o[t], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w.part[i], o[t], 0, 0, 0);
     }
   } else {
 #pragma unroll
@@ -129,23 +146,28 @@ __device__ __forceinline__ void paged_values(const typename PagedGeo<T, D>::Vecs
 
 // The same for the rows of one new token alone (`mine`), of the tokens of `keep` (bit e:
 // this lane's token 8 (lane / 16) + e): the others' values, which may be infinite or NaN,
-// are left out.  bf16: weights of 8 bits, of which none is 0 beside an infinite value.
+// are left out.  bf16: infinite and NaN values only times a weight's first part, which is 0
+// only if the weight is (the others may be 0, or negative).
 template <typename T, int D>
 __device__ __forceinline__ void paged_values_of(const typename PagedGeo<T, D>::Vecs& vw, const float (&p)[8], uint32_t keep,
                                                 bool mine, pa_f32x4 (&o)[D / 16]) {
   constexpr int DT = D / 16;
   if constexpr (T::kBytes == 2) {
-    pa_bf16x8 hi;
+    const PagedWeights w(p);
     u32x4 m;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) hi[e] = (__bf16)p[e];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       m[e] = ((keep >> (2 * e)) & 1u ? 0xFFFFu : 0u) | ((keep >> (2 * e + 1)) & 1u ? 0xFFFF0000u : 0u);
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
-      const pa_f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pa_bf16x8, vw[t] & m), hi,
-                                                                 pa_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      u32x4 v = vw[t] & m;
+      pa_f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pa_bf16x8, v), w.part[0], x, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = paged_finite(v[e]);
+#pragma unroll
+      for (int i = 1; i < 3; ++i)
+        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pa_bf16x8, v), w.part[i], x, 0, 0, 0);
       if (mine) o[t] += x;
     }
   } else {

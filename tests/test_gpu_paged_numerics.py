@@ -1,0 +1,77 @@
+"""What attention over a cache in pages keeps of its numbers: the softmax weights' bits,
+fp32's, and what infinite scores give, against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as O
+from paper_2410_18701_amd.paged import PagedCache
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+PATHS = [(1, 1), (5, 2), (16, 1), (16, 2), (16, 4)]      # width, query heads a kv-head: 1 to 64 rows
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def attend(k, v, q, k_new, v_new, dtype, scale=0.0, page=32):
+    """One query: cached k, v [hkv][n][d], new ones [t][hkv][d], q [t][hq][d], all float64 arrays that
+    the type holds -> (out, what 64 bits give), [t][hq][d]."""
+    t, hq, d = q.shape
+    hkv, n = k.shape[:2]
+    dev = lambda x: torch.tensor(x, device="cuda").to(DT[dtype]).contiguous()  # noqa: E731
+    c = PagedCache(1, 1, hq, hkv, d, 8 + (n + t) // page, 8 + (n + t) // page, page=page, width=t, dtype=dtype)
+    c.kv.fill_(float("nan"))
+    c.begin(i32([n]))
+    c.embed([0], [n], [dev(k[None])], [dev(v[None])])
+    c.begin(i32([t]), keep=i32([n]))
+    out = c.decode_attn(0, dev(q[None]), dev(k_new[None]), dev(v_new[None]), scale=scale)
+    with np.errstate(invalid="ignore"):
+        want = O.attention(q, np.concatenate([k, k_new.transpose(1, 0, 2)], 1),
+                           np.concatenate([v, v_new.transpose(1, 0, 2)], 1), n, scale=scale or None)
+    return f64(out)[0], want
+
+
+def bf16(x):
+    return f64(torch.tensor(x).bfloat16())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [None, float("inf"), float("nan")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("width,group", PATHS)
+def test_weights_keep_their_bits(width, group, d, bad, dtype):
+    """Three tokens of weights 1, 1 and p = exp(-n / 16) whose values cancel but for their last bits:
+    a weight's rounding is all that is left.  Scores are whole numbers.  Off by, in units of 2^-23:
+    p < 1 times a value below 2 by 4 (the exponential 2^-23 of it, its argument 2^-24, the scale 2^-25
+    of at most 1.2), the weights of 1 by 2, sums of numbers below 2 in at most three products 6; all
+    that over a sum of weights of at least 2: 6 2^-23 < 2^-20.  (A weight of 16 bits is off by up to
+    2^-18 of itself, here 2^-18.8.)  An infinite or NaN value in one column takes nothing from the others."""
+    rng = np.random.default_rng(width + group)
+    ns = (1, 2, 3, 5, 7, 9, 11, 13)
+    hkv = len(ns)
+    qh, k_a = rng.integers(-2, 3, (hkv, d)).astype(float), rng.integers(-2, 3, (hkv, d)).astype(float)
+    qh[:, 0] = 1
+    k = np.repeat(k_a[:, None], 3, 1)
+    k[:, 1, 0] -= ns
+    p = np.exp(-np.array(ns) / 16)[:, None]
+    v_b = bf16(rng.uniform(1, 2, (hkv, d)) * rng.choice([-1, 1], (hkv, d)))
+    v_a = -bf16(p * v_b)
+    v = np.stack([v_a, v_b, -bf16(p * v_b + v_a)], 1)
+    if bad is not None:
+        v[:, 1, 5] = bad
+    q = np.broadcast_to(np.repeat(qh, group, 0), (width, hkv * group, d))
+    k_new = np.broadcast_to(-100 * np.sign(qh), (width, hkv, d))          # scores below -3000: no weight
+    out, want = attend(k, v, q, k_new, np.broadcast_to(v_b, (width, hkv, d)), dtype, scale=1 / 16)
+    if bad is not None:
+        assert np.array_equal(out[..., 5], want[..., 5], equal_nan=True)
+        out, want = np.delete(out, 5, 2), np.delete(want, 5, 2)
+    err = np.abs(out - want) - (2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0.0)
+    assert err.max() <= 2.0 ** -20, err.max()
