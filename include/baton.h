@@ -644,8 +644,9 @@ baton_status baton_paged_reset(const baton_paged_desc* desc, const int32_t* orde
 /*
  * Ends the last step and begins the next.  keep, n_new: device arrays of batch entries.
  * Of slot b's tokens those stay that it had before the last step and the first keep[b]
- * of that step's new ones (NULL: none of them); keep[b] < 0: its query leaves, the slot is free, its
- * pages go back.  Then n_new[b] new tokens (< 1: none) are provided for: pages for
+ * of that step's new ones (NULL: none of them; more than there are: all; none of a slot
+ * that took no part in it); keep[b] < 0: its query leaves, the slot is free, its pages go
+ * back.  Then n_new[b] new tokens (< 1: none) are provided for: pages for
  * lens[b] + n_new[b] tokens in all are in the table, pages past that go back to the
  * pool (what was drafted and not kept), and so do those behind the window.
  * Pages go back before any are taken, and are taken by the slots in order: a slot
@@ -701,8 +702,8 @@ size_t baton_paged_attn_workspace_bytes(const baton_paged_desc* desc, int32_t wi
  * [batch][width][n_q_heads][head_dim].  Rows of out past a slot's new tokens are not
  * written.  What a token does not see -- the tokens behind it, those outside the
  * window, what else its pages hold -- has no influence, whatever its bits.  fp32
- * arithmetic (softmax weights among it), out rounded to nearest even.  scale = 0 selects 1/sqrt(head_dim).  A step may be repeated: the same calls give the
- * same bits.
+ * arithmetic (softmax weights among it), out rounded to nearest even.  scale = 0 selects
+ * 1/sqrt(head_dim).  A step may be repeated: the same calls give the same bits.
  * ws: baton_paged_attn_workspace_bytes, 16-byte aligned; nothing is kept there between
  * calls, but calls that share one go to one stream.
  * Errors: EINVAL also for a layer out of range, one of k_new and v_new alone, a

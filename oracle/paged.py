@@ -12,7 +12,7 @@ class Tables:
         self.table = [[-1] * max_pages for _ in range(batch)]
         self.lens = [0] * batch
         self.upto = [0] * batch      # blocks handed out (those given back behind the window among them)
-        self.n_new = [0] * batch
+        self.n_new = [0] * batch     # new tokens of the last step (0 where pages were lacking)
 
     def step(self, n_new, keep=None, width=1):
         """Returns (slot_map, missing)."""
@@ -28,7 +28,7 @@ class Tables:
                 self.upto[b] = 0
                 want[b] = -(-max(0, int(n_new[b])) // P)
             else:
-                self.lens[b] = min(self.lens[b] + k, self.upto[b] * P)
+                self.lens[b] += min(k, self.n_new[b])
                 want[b] = -(-(self.lens[b] + max(0, int(n_new[b]))) // P)
                 low = self.lens[b] - self.window + 1 if self.window else 0     # the first token the window shows
                 gone = [j for j in range(self.upto[b])

@@ -133,10 +133,9 @@ __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedSte
     released = a.state[a.at.released + b];
     const int32_t keep = a.keep ? a.keep[b] : 0;
     fresh = max(a.n_new[b], 0);
+    const int32_t took = a.state[a.at.n_new + b];     // new tokens of the last step, 0 if it had no pages
     leaves = keep < 0;
-    // tokens without a page are not kept
-    const int64_t l = (int64_t)max(a.lens[b], 0) + keep, most = (int64_t)covered << a.page_shift;
-    len = leaves ? 0 : (int32_t)(l < most ? l : most);
+    len = leaves ? 0 : max(a.lens[b], 0) + min(keep, took);
   }
   // Blocks of pages that stay in front of the window, and those that the window has left.
   const int32_t s0 = (a.sinks + page - 1) >> a.page_shift;

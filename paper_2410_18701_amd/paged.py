@@ -64,8 +64,9 @@ class PagedCache:
         B.baton_paged_reset(self.desc, order, _cur_stream())
 
     def begin(self, n_new, keep=None):
-        """Ends the last step (keep [batch]: how many of its new tokens stay, < 0: the query
-        leaves; None: none stay) and begins the next with n_new [batch] new tokens; returns slot_map."""
+        """Ends the last step (keep [batch]: how many of its new tokens stay, of a slot that lacked
+        pages none whatever it says, < 0: the query leaves; None: none stay) and begins the next
+        with n_new [batch] new tokens; returns slot_map."""
         self._numbers("n_new", n_new, self.batch)
         if keep is not None:
             self._numbers("keep", keep, self.batch)
