@@ -659,7 +659,8 @@ baton_status baton_paged_reset(const baton_paged_desc* desc, const int32_t* orde
  * order of (slot, block) from its top, and the k-th one taken, in the same order, is
  * the k-th from the top.  A prompt is a step too: n_new its length, then
  * baton_paged_embed; attention leaves slots with more than its width alone.
- * Errors: EINVAL also for null n_new, width outside 1 .. 2^20 or map_ld < width with a slot_map.
+ * Errors: EINVAL also for null n_new, and with a slot_map for width outside 1 .. 2^20 or
+ * map_ld outside width .. 2^40.
  */
 baton_status baton_paged_step(const baton_paged_desc* desc, const int32_t* keep, const int32_t* n_new,
                               int32_t* slot_map, int32_t width, int64_t map_ld, int32_t* missing, hipStream_t stream);

@@ -164,7 +164,7 @@ baton_status baton_paged_step(const baton_paged_desc* d, const int32_t* keep, co
   if (st != BATON_OK) return st;
   if (!n_new || !aligned(n_new, 4) || !aligned(keep, 4) || !aligned(slot_map, 4) || !aligned(missing, 4))
     return BATON_EINVAL;
-  if (slot_map && (width < 1 || width > (1 << 20) || map_ld < width)) return BATON_EINVAL;
+  if (slot_map && (width < 1 || width > (1 << 20) || map_ld < width || map_ld > (int64_t(1) << 40))) return BATON_EINVAL;
   baton::PagedStepArgs a;
   std::memset(&a, 0, sizeof(a));
   a.table = d->table;

@@ -74,7 +74,8 @@ struct PagedStepArgs {
   const int32_t* n_new;
   int32_t* slot_map;        // null: not wanted
   int32_t* missing;         // null: not wanted
-  int32_t batch, max_pages, page_shift, window, sinks, n_kv_heads, group, width, map_ld;
+  int64_t map_ld;
+  int32_t batch, max_pages, page_shift, window, sinks, n_kv_heads, group, width;
   PagedState at;
 };
 
@@ -248,7 +249,7 @@ __global__ void __launch_bounds__(kStepThreads) paged_step_kernel(const PagedSte
       const int32_t id = a.table[(int64_t)s * a.max_pages + (t >> a.page_shift)];
       place = id < 0 ? -1 : (id << a.page_shift) + (int32_t)(t & (page - 1));
     }
-    a.slot_map[(int64_t)s * a.map_ld + i] = place;
+    a.slot_map[s * a.map_ld + i] = place;
   }
 }
 
