@@ -589,7 +589,7 @@ baton_status baton_sample(int32_t dtype, const void* logits, int64_t ld, int32_t
  * whole steps are enqueued, or captured into a graph, without waiting for the host.
  *
  * A step: baton_paged_step (ends the last step, hands out pages), then for each layer
- * baton_paged_attn, then e.g. baton_verify, whose n_out is the next step's keep.
+ * baton_paged_attn, then e.g. baton_paged_verify, whose n_out is the next step's keep.
  *
  * With window > 0 a new token at position p sees the tokens j with p - window < j <= p
  * and those with j < sinks (the first tokens stay visible), else all j <= p.  Pages
@@ -751,6 +751,22 @@ baton_status baton_verify(int32_t dtype, const void* target, int64_t target_ld, 
                           const float* u_accept, const float* u_token, const float* temperature, const int32_t* top_k,
                           const float* top_p, const float* min_p, int32_t* tokens, int32_t* n_out, void* ws,
                           size_t ws_bytes, hipStream_t stream);
+
+/*
+ * baton_verify of the drafts of a paged cache's present step (the last baton_paged_step of
+ * the stream), batch being desc's.  A slot of which the step took no tokens -- it lacked
+ * pages, or n_new was below 1 -- or more than width (a prompt) is a free one, whatever
+ * n_draft says: its rows of target hold nothing of it.  The others have at most the drafts
+ * that the step took, n_new - 1 (n_draft NULL: as many).  So n_out is what the cache keeps, and a
+ * slot that lacked pages brings the same tokens again in a later step.
+ * Errors: those of both.
+ */
+baton_status baton_paged_verify(const baton_paged_desc* desc, int32_t dtype, const void* target, int64_t target_ld,
+                                const void* draft, int64_t draft_ld, int32_t width, int32_t vocab,
+                                const int32_t* drafted, const int32_t* n_draft, const float* u_accept,
+                                const float* u_token, const float* temperature, const int32_t* top_k,
+                                const float* top_p, const float* min_p, int32_t* tokens, int32_t* n_out, void* ws,
+                                size_t ws_bytes, hipStream_t stream);
 
 /* Static English text of a status. */
 const char* baton_status_string(baton_status status);

@@ -120,6 +120,7 @@ def lib():
         L.baton_verify_workspace_bytes.argtypes = [i32, i32, i32]
         L.baton_verify_workspace_bytes.restype = sz
         L.baton_verify.argtypes = [i32, vp, i64, vp, i64, i32, i32, i32] + [vp] * 11 + [sz, vp]
+        L.baton_paged_verify.argtypes = [pd, i32, vp, i64, vp, i64, i32, i32] + [vp] * 11 + [sz, vp]
         L.baton_status_string.argtypes = [st]
         L.baton_status_string.restype = ctypes.c_char_p
         for name in ("baton_cache_create", "baton_cache_destroy", "baton_kv_evict", "baton_kv_embed",
@@ -130,7 +131,7 @@ def lib():
                      "baton_linear_packed_rmsnorm", "baton_linear_packed_silu",
                      "baton_rmsnorm", "baton_rope_qkv", "baton_silu_mul", "baton_linear_adapters", "baton_sample",
                      "baton_paged_reset", "baton_paged_step", "baton_paged_embed", "baton_paged_extract",
-                     "baton_paged_rope_qkv", "baton_paged_attn", "baton_verify"):
+                     "baton_paged_rope_qkv", "baton_paged_attn", "baton_verify", "baton_paged_verify"):
             getattr(L, name).restype = st
         _lib = L
     return _lib
@@ -395,3 +396,11 @@ def baton_verify(dtype, target, target_ld, draft, draft_ld, batch, width, vocab,
                               _ptr(n_draft), _ptr(u_accept), _ptr(u_token), _ptr(temperature), _ptr(top_k), _ptr(top_p),
                               _ptr(min_p), _ptr(tokens), _ptr(n_out), _ptr(ws), ws_bytes, _stream(stream)),
            "baton_verify")
+
+
+def baton_paged_verify(desc, dtype, target, target_ld, draft, draft_ld, width, vocab, drafted, n_draft, u_accept, u_token,
+                       temperature, top_k, top_p, min_p, tokens, n_out, ws, ws_bytes, stream=None):
+    _check(lib().baton_paged_verify(ctypes.byref(desc), dtype, _ptr(target), target_ld, _ptr(draft), draft_ld, width, vocab,
+                                    _ptr(drafted), _ptr(n_draft), _ptr(u_accept), _ptr(u_token), _ptr(temperature),
+                                    _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(tokens), _ptr(n_out), _ptr(ws), ws_bytes,
+                                    _stream(stream)), "baton_paged_verify")

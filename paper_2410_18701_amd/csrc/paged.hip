@@ -11,6 +11,7 @@
 #include "layer_ops.hpp"
 #include "paged_attn.hpp"
 #include "paged_ops.hpp"
+#include "verify.hpp"
 
 namespace {
 
@@ -273,6 +274,19 @@ baton_status baton_paged_attn(const baton_paged_desc* d, int32_t layer, const vo
     else launch_attn<baton::BF16Tag, 128>(a, items, split, stream);
   }
   return done();
+}
+
+baton_status baton_paged_verify(const baton_paged_desc* d, int32_t dtype, const void* target, int64_t target_ld,
+                                const void* draft, int64_t draft_ld, int32_t width, int32_t vocab,
+                                const int32_t* drafted, const int32_t* n_draft, const float* u_accept,
+                                const float* u_token, const float* temperature, const int32_t* top_k,
+                                const float* top_p, const float* min_p, int32_t* tokens, int32_t* n_out, void* ws,
+                                size_t ws_bytes, hipStream_t stream) {
+  const baton_status st = check(d);
+  if (st != BATON_OK) return st;
+  return baton::verify(d->state + state_at(*d).n_new, dtype, target, target_ld, draft, draft_ld, d->batch, width, vocab,
+                       drafted, n_draft, u_accept, u_token, temperature, top_k, top_p, min_p, tokens, n_out, ws,
+                       ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -48,6 +48,7 @@ struct VerifyArgs {
   int32_t batch, width, vocab, shift, segs, per_part;   // per_part: tokens of a wave's part of a segment
   const int32_t* drafted;      // [batch][width - 1]
   const int32_t* n_draft;      // [batch]; null: width - 1
+  const int32_t* taken;        // [batch] new tokens that the cache's step took; null: those that n_draft says
   const float* u_accept;       // [batch][width - 1]
   const float* u_token;        // [batch]
   const float* temperature;    // [batch] each; null: 1, off, off, off
@@ -62,8 +63,13 @@ struct VerifyArgs {
   int32_t n_pieces, slot_rows; // rows of a slot: width, and width - 1 with a draft's logits
 };
 
+// A slot's drafts, negative if it takes no part: also where the cache's step took none of its
+// tokens, or more of them (a prompt's) than there are rows.
 __device__ __forceinline__ int32_t verify_drafts(const VerifyArgs& a, int32_t b) {
-  return a.n_draft ? min(a.n_draft[b], a.width - 1) : a.width - 1;
+  const int32_t n = a.n_draft ? min(a.n_draft[b], a.width - 1) : a.width - 1;
+  if (!a.taken) return n;
+  const int32_t t = a.taken[b];
+  return t < 1 || t > a.width ? -1 : min(n, t - 1);
 }
 
 // A slot's row i: of the target's, then of the draft's.  False if it is not needed.

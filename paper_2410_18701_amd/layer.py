@@ -233,10 +233,12 @@ class Verifier:
         return t.stride(1) if n > 1 else t.stride(0) if b > 1 else self.vocab
 
     def __call__(self, target, draft, drafted, n_draft, u_accept, u_token, temperature=None, top_k=None, top_p=None,
-                 min_p=None):
+                 min_p=None, cache=None):
         """target [batch][width][vocab], draft [batch][width - 1][vocab] (or None: the drafts are
         tokens without a distribution), fp32 or bf16; drafted int32 and u_accept [batch][width - 1];
-        n_draft int32 [batch] (None: all; negative: a free slot); u_token [batch]."""
+        n_draft int32 [batch] (None: all; negative: a free slot); u_token [batch].  cache: the
+        PagedCache whose present step the drafts belong to, of which slots that took no part in
+        it (they lacked pages) are free ones, and others have at most the drafts that it took."""
         import torch
         b, w = self.batch, self.width
         dtype = {torch.float32: B.BATON_F32, torch.bfloat16: B.BATON_BF16}.get(target.dtype)
@@ -256,10 +258,16 @@ class Verifier:
                 continue
             if t is None or t.dtype != want or t.numel() != n or not t.is_contiguous():
                 raise ValueError(f"Verifier: {name} must be {n} contiguous {want} values")
+        if cache is not None and cache.batch != b:
+            raise ValueError(f"Verifier: a cache of {cache.batch} slots, not {b}")
         _on_this_gpu("Verifier", self.ws, target, draft, drafted, n_draft, u_accept, u_token, temperature, top_k, top_p,
-                     min_p)
-        B.baton_verify(dtype, target, target_ld, draft, draft_ld, b, w, self.vocab, drafted, n_draft, u_accept, u_token,
-                       temperature, top_k, top_p, min_p, self.tokens, self.n_out, self.ws, self.ws_bytes, _stream())
+                     min_p, None if cache is None else cache.lens)
+        rest = (w, self.vocab, drafted, n_draft, u_accept, u_token, temperature, top_k, top_p, min_p, self.tokens,
+                self.n_out, self.ws, self.ws_bytes, _stream())
+        if cache is None:
+            B.baton_verify(dtype, target, target_ld, draft, draft_ld, b, *rest)
+        else:
+            B.baton_paged_verify(cache.desc, dtype, target, target_ld, draft, draft_ld, *rest)
         return self.tokens, self.n_out
 
 
@@ -353,7 +361,7 @@ class DecodeLayers:
 
     def next_tokens(self, x, u, temperature=None, top_k=None, top_p=None, min_p=None):
         """The next token of every slot (int32 [batch], the Sampler's own tensor; a free
-        slot's says nothing) from the last layer's residual stream x [batch][hid]: norm,
+        slot's, or one's that lacked pages, says nothing) from the last layer's residual stream x [batch][hid]: norm,
         vocabulary projection, sampling with each slot's parameters and random number u."""
         if self.head is None or self.sampler is None:
             raise ValueError("next_tokens: no head was given" if self.head is None else
@@ -370,8 +378,11 @@ class DecodeLayers:
         """Over a PagedCache: the drafted tokens that are accepted and the token behind them
         (tokens [batch][width], n_out [batch], the Verifier's own tensors) from the last layer's
         residual stream x [batch * width][hid], whose row b width + i belongs to slot b's i-th
-        new token; the other arguments as Verifier's.  n_out is the next begin's keep."""
+        new token; the other arguments as Verifier's.  n_out is the next begin's keep: 0, with no
+        tokens, of a slot that took no part in the step, which brings its tokens again once
+        the pool has pages."""
         if self.head is None or self.verifier is None:
             raise ValueError("accept_drafts: no head was given" if self.head is None else "accept_drafts: a PagedCache only")
         logits = self._logits(x).view(self.cache.batch, self.width, -1)
-        return self.verifier(logits, draft, drafted, n_draft, u_accept, u_token, temperature, top_k, top_p, min_p)
+        return self.verifier(logits, draft, drafted, n_draft, u_accept, u_token, temperature, top_k, top_p, min_p,
+                             cache=self.cache)
