@@ -301,7 +301,7 @@ struct PagedTile {
       // large (the reference's own rounding is the same for all tokens); in fp32 with the rest
       // of the scale, which is off by up to 2^-25 of itself.
       float x = fmaf(s[e], r.qscale, -ref);
-      if constexpr (T::kBytes == 4) x = fmaf(s[e], r.qscale_rest, x);
+      if constexpr (T::kBytes == 4) x = x == -INFINITY ? x : fmaf(s[e], r.qscale_rest, x);   // (inf - inf where the signs differ)
       p[e] = (bits >> e) & 1u ? fast_exp2(x) : 0.f;
       sum += p[e];
     }

@@ -75,3 +75,50 @@ def test_weights_keep_their_bits(width, group, d, bad, dtype):
         out, want = np.delete(out, 5, 2), np.delete(want, 5, 2)
     err = np.abs(out - want) - (2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0.0)
     assert err.max() <= 2.0 ** -20, err.max()
+
+
+def normal(rng, dtype, *shape):
+    x = rng.normal(size=shape)
+    return bf16(x) if dtype == "bf16" else x.astype(np.float32).astype(np.float64)
+
+
+def close(out, want, vmax, dtype):
+    """As the other tests of this attention: 2^-12 of the largest value, bf16 half a step more."""
+    assert np.array_equal(np.isnan(out), np.isnan(want))
+    err = np.where(np.isnan(want), 0.0, np.abs(out - want)) - 2.0 ** -12 * vmax
+    assert (err <= (2.0 ** -8 * np.abs(np.nan_to_num(want)) if dtype == "bf16" else 0.0)).all()
+
+
+LENS_AND_PATHS = [(41, p) for p in PATHS] + [(9000, PATHS[0]), (9000, PATHS[3])]      # 9,000: several work items
+SCALES = [(64, 0.0), (128, 0.0), (64, -0.2), (128, -0.3)]
+
+
+def with_infinities(n, width, group, d, scale, dtype, keys, new_keys):
+    """Query, keys and values of four kv-heads; keys(k, low), new_keys(k_new, low) put `low`, which gives a
+    score of -inf, into some keys."""
+    rng = np.random.default_rng(d + width)
+    low = float("-inf") if scale >= 0 else float("inf")
+    q, k, v = (normal(rng, dtype, *s) for s in ((width, 4 * group, d), (4, n, d), (4, n, d)))
+    k_new, v_new = (normal(rng, dtype, width, 4, d) for _ in range(2))
+    q[..., 0] = 1
+    keys(k[..., 0], low)
+    new_keys(k_new[..., 0], low)
+    return attend(k, v, q, k_new, v_new, dtype, scale=scale) + (np.abs(v).max(),)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,scale", SCALES)
+@pytest.mark.parametrize("n,path", LENS_AND_PATHS)
+def test_scores_of_minus_infinity(n, path, d, scale, dtype):
+    """Weight 0 where the score is -inf, as the formula has it: every second token of kv-head 0, all but one of
+    kv-head 1, new ones of kv-head 2; a score of +inf in kv-head 3 is NaN."""
+    def keys(k, low):
+        k[0, ::2] = k[1, :-1] = low
+        k[3, 5] = -low
+
+    def new_keys(k, low):
+        k[:, 1:3] = low
+
+    out, want, vmax = with_infinities(n, *path, d, scale, dtype, keys, new_keys)
+    assert np.isnan(want).sum() == want.size / 4
+    close(out, want, vmax, dtype)
