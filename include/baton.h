@@ -703,7 +703,8 @@ size_t baton_paged_attn_workspace_bytes(const baton_paged_desc* desc, int32_t wi
  * [batch][width][n_q_heads][head_dim].  Rows of out past a slot's new tokens are not
  * written.  What a token does not see -- the tokens behind it, those outside the
  * window, what else its pages hold -- has no influence, whatever its bits.  fp32
- * arithmetic (softmax weights among it), out rounded to nearest even.  scale = 0 selects
+ * arithmetic (softmax weights among it), out rounded to nearest even; where all scores are
+ * -inf, or one is +inf or NaN, NaN.  scale = 0 selects
  * 1/sqrt(head_dim).  A step may be repeated: the same calls give the same bits.
  * ws: baton_paged_attn_workspace_bytes, 16-byte aligned; nothing is kept there between
  * calls, but calls that share one go to one stream.

@@ -327,7 +327,7 @@ __device__ __forceinline__ void paged_write(const PagedAttnArgs& a, const PagedI
   const int32_t G = a.group, r = x.first + c16;
   if (r >= it.n_new * G) return;
   if (it.parts == 1) {
-    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
+    const float inv = 1.f / x.l;       // (every score -inf: NaN)
     uint8_t* const row = a.out + ((((int64_t)it.b * a.width + r / G) * a.n_kv_heads + h) * G + r % G) * Geo::kRow;
 #pragma unroll
     for (int t = 0; t < Geo::kDt; ++t) {
@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnArgs 
     o += *reinterpret_cast<const pa_f32x4*>(sm_o[v] + 4 * d4);
     sum += sm_l[v];
   }
-  const pa_f32x4 x = o * (sum == 0.f ? 0.f : 1.f / sum);
+  const pa_f32x4 x = o * (1.f / sum);
   uint8_t* const row = a.out + ((((int64_t)b * a.width + r / G) * a.n_kv_heads + h) * G + r % G) * Geo::kRow;
   if constexpr (T::kBytes == 2)
     *reinterpret_cast<uint2*>(row + 8 * d4) = make_uint2(f32_to_bf16_rne(x[0]) | f32_to_bf16_rne(x[1]) << 16,

@@ -122,3 +122,20 @@ def test_scores_of_minus_infinity(n, path, d, scale, dtype):
     out, want, vmax = with_infinities(n, *path, d, scale, dtype, keys, new_keys)
     assert np.isnan(want).sum() == want.size / 4
     close(out, want, vmax, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,scale", SCALES)
+@pytest.mark.parametrize("n,path", LENS_AND_PATHS)
+def test_rows_of_minus_infinity_alone(n, path, d, scale, dtype):
+    """Where every score is -inf there is nothing to divide by: NaN, as the formula has it.  kv-head 0: all
+    tokens; 1: all but the first; 2: all but the new ones; 3: the new ones."""
+    def keys(k, low):
+        k[0] = k[2] = k[1, 1:] = low
+
+    def new_keys(k, low):
+        k[:, [0, 1, 3]] = low
+
+    out, want, vmax = with_infinities(n, *path, d, scale, dtype, keys, new_keys)
+    assert np.isnan(want).sum() == want.size / 4
+    close(out, want, vmax, dtype)
