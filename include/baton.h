@@ -710,7 +710,7 @@ size_t baton_paged_attn_workspace_bytes(const baton_paged_desc* desc, int32_t wi
  * calls, but calls that share one go to one stream.
  * Errors: EINVAL also for a layer out of range, one of k_new and v_new alone, a
  * misaligned pointer, width outside 1 .. BATON_PAGED_MAX_WIDTH or width * n_q_heads / n_kv_heads >
- * BATON_PAGED_MAX_ROWS, a scale that is not finite, ws too small.
+ * BATON_PAGED_MAX_ROWS, a scale above 2^127 in magnitude or NaN, ws too small.
  */
 baton_status baton_paged_attn(const baton_paged_desc* desc, int32_t layer, const void* q, const void* k_new,
                               const void* v_new, int32_t width, void* out, float scale, void* ws, size_t ws_bytes,

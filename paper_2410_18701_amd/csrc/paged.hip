@@ -230,7 +230,8 @@ baton_status baton_paged_attn(const baton_paged_desc* d, int32_t layer, const vo
   const baton_status st = check(d);
   if (st != BATON_OK) return st;
   const int32_t group = d->n_q_heads / d->n_kv_heads;
-  if (layer < 0 || layer >= d->n_layers || !q || !out || !k_new != !v_new || !std::isfinite(scale)) return BATON_EINVAL;
+  if (layer < 0 || layer >= d->n_layers || !q || !out || !k_new != !v_new || !(std::fabs(scale) <= 0x1p127f))
+    return BATON_EINVAL;                   // (times log2 e it is finite)
   if (width < 1 || width > BATON_PAGED_MAX_WIDTH || width * group > BATON_PAGED_MAX_ROWS) return BATON_EINVAL;
   if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(out, 16)) return BATON_EINVAL;
   const size_t need = baton_paged_attn_workspace_bytes(d, width);
