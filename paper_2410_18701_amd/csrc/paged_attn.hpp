@@ -24,7 +24,8 @@
 // a second launch.
 //
 // Errors, relative to 64 bits (random lengths, windows and drafts): fp32 2.2e-7, where
-// torch's products and softmax have 4.7e-7; bf16 1.7e-3 as theirs, the result's rounding.
+// torch's products and softmax have 4.7e-7; bf16 1.7e-3 as theirs, the result's rounding,
+// which falls the other way than theirs in one of 10,000 (5e-5 of the outputs' size).
 #pragma once
 
 #include "paged_ops.hpp"
@@ -94,7 +95,11 @@ __device__ __forceinline__ void paged_scores(const typename PagedGeo<T, D>::Vecs
   }
 }
 
-// fp32 weights as three bf16 numbers each, of 8 bits: their sum is the weight.
+// fp32 weights as three bf16 numbers each, of 8 bits: their sum is the weight.  The third
+// product of a block's values costs steps of up to 16 rows nothing that shows (32 slots of up
+// to 2,048 tokens 104.9 us, with two 104.7; 64 of up to 8,192, two layers, 401.9 and 401.1),
+// 32 slots with four drafts each over up to 32,768 tokens 51.3 us instead of 49.4.  With two,
+// 16 bits, the first one's results were 1.0e-4 of their size from those of fp32 weights, now 5e-5.
 struct PagedWeights {
   pa_bf16x8 part[3];
 
@@ -467,9 +472,10 @@ __device__ __forceinline__ void paged_wait_loads() { __builtin_amdgcn_s_waitcnt(
 // An item of up to 16 rows.  Every wave has all of them, and every fourth of the item's
 // blocks, whose keys and values go from memory into its registers: 1 KB of consecutive bytes
 // per load, no LDS and no barrier until the merge.  Bound by memory: 64 slots of up to 8,192
-// tokens (64/8 heads, bf16) take 193 us a layer, 5.9 TB/s of 6.09 that a plain read of that
-// size reaches; 32 of up to 2,048 (32/32 heads) 98 us, 5.8 TB/s.  The matrix cores are busy a
-// quarter of the time.
+// tokens (64/8 heads, bf16) take 194 us a layer, 5.9 TB/s of 6.09 that a plain read of that
+// size reaches, with two new tokens each 201; 32 of up to 2,048 (32/32 heads) 100 us, 5.7 TB/s.
+// The matrix cores are busy a third of the time.  bf16 at head_dim 64 5.9 TB/s, fp32 5.3 at 64
+// and 5.0 at 128 (64 of up to 4,096 tokens, 64/8 heads).
 template <typename T, int D>
 __device__ __forceinline__ void paged_item16(const PagedAttnArgs& a, const PagedItem& it, int32_t item, int32_t h,
                                              const PagedRows& r, u32x4 (*sm)[kWave], float (*sm_m)[16], float (*sm_l)[16]) {
@@ -547,12 +553,13 @@ __device__ __forceinline__ void paged_load_lds(const uint8_t* from, uint32_t l16
 // An item of more than 16 rows, up to 64: blocks go from memory into LDS, without registers, a
 // pair of them while the last pair is worked on, and the waves share them: with more than 32
 // rows each wave has a tile of its own, with 32 two waves share a tile and a pair.  32 slots
-// with four drafts each (32/4 heads, lengths up to 32,768, most far shorter): 50 us a step,
+// with four drafts each (32/4 heads, lengths up to 32,768, most far shorter): 51 us a step,
 // whose bytes take 32.  Waves wait for loads 3% of the loop; it is bound by a tile's chain of
-// product, maximum, exponential and product, some 2,800 cycles a block with a barrier at each
-// (58 us, three blocks ahead; 56 with two), which a pair's two chains overlap (52, and 50
-// with items of up to 16 rows as above, which all of a call's items took here before: 131 us
-// instead of 105 for the 32 slots of up to 2,048, 470 instead of 400 for two layers of the 64).
+// product, maximum, exponential and product.  Before weights had three parts: some 2,800 cycles
+// a block with a barrier at each (58 us, three blocks ahead; 56 with two), which a pair's two
+// chains overlap (52, and 49 with items of up to 16 rows as above, which all of a call's items
+// took here before: 131 us instead of 105 for the 32 slots of up to 2,048, 470 instead of 400
+// for two layers of the 64).
 //
 // Two waves a SIMD are asked for (fp32 at head_dim 128, whose blocks are twice as large: one),
 // which leaves registers for K and V of a block each; with all of a SIMD's registers for one
@@ -656,8 +663,8 @@ paged_attn_kernel(const PagedAttnArgs a) {
 
 // Rows of slots with several work items: their partial sums.  One workgroup per (slot,
 // head) and row; D / 4 threads hold the columns, the others' groups take every
-// 256 / (D / 4)-th item, and their sums are added in order.  Bound by latency: 3.9 to 6.9 us,
-// of which a launch is 3.4.
+// 256 / (D / 4)-th item, and their sums are added in order.  Bound by latency: 3.5 to 6.9 us
+// with few rows, of which a launch is 3.4, 12 with 16 rows a head of 64 slots.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) paged_combine_kernel(const PagedAttnArgs a) {
   using Geo = PagedGeo<T, D>;

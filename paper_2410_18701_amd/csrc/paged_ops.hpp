@@ -19,17 +19,20 @@ namespace baton {
 
 constexpr int kPagedBlock = 32;          // tokens per block
 constexpr int kPagedMaxNew = 16;         // == BATON_PAGED_MAX_WIDTH
-// Workgroups of an attention launch, about, and blocks per work item, at least.  Two
-// workgroups fit a compute unit, 512 the GPU.
+// Workgroups of an attention launch, about, and blocks per work item, at least.  A compute
+// unit holds two workgroups of bf16 at head_dim 128 and of fp32 at 64 (512 on the GPU), three
+// of bf16 at 64, one of fp32 at 128; the step, which makes the items, knows neither type nor
+// head_dim, and the numbers are those that served the first best.
 //  * Up to 16 rows per head, 2048: four rounds even out lengths, and every item costs its
 //    start and its part of the second launch.  With 1024, 2048 and 4096 a step of 32 slots
-//    of up to 2,048 tokens (32/32 heads) took 113, 105 and 102 us, two layers of 64 slots of
-//    up to 8,192 (64/8 heads) 399, 400 and 411.
-//  * More rows, 512: an item's start (its loads into LDS, its merge) is longer.  32 slots
-//    of very different lengths up to 32,768 (32/4 heads) with four drafts each: 51.4 us
-//    with 448, 49.9 with 512, 57.5 with 640 and 53.6 with 1024.
+//    of up to 2,048 tokens (32/32 heads) took 112, 104 and 103 us, two layers of 64 slots of
+//    up to 8,192 (64/8 heads) 400, 401 and 413.
+//  * More rows, 512, for all of a call's items if any slot has more: an item's start (its
+//    loads into LDS, its merge) is longer.  32 slots of very different lengths up to 32,768
+//    (32/4 heads) with four drafts each: 53.3 us with 448, 51.7 with 512, 59.4 with 640 and
+//    55.8 with 1024, by how full the last round of workgroups is.
 //  * 8 blocks, two a wave.  With 4, 8 and 16 a step of four slots of up to 128 tokens took
-//    14.3, 11.1 and 10.5 us, one of seven in fp32 with a window of 333 12.7, 12.9 and 16.8.
+//    13.6, 11.3 and 10.9 us, one of seven in fp32 with a window of 333 13.3, 13.8 and 15.9.
 constexpr int kPagedItems = 2048;
 constexpr int kPagedRowItems = 512;      // more than 16 rows
 constexpr int kPagedMinBlocks = 8;
